@@ -327,6 +327,89 @@ fma_status_t fma_backward_linear(fma_plan_t plan, const void *q, const void *k, 
 fma_status_t fma_forward_static(fma_plan_t plan, const void *q, const void *k, const void *v,
                                 const float *wk, const float *wv, void *out, void *stream);
 
+/* ------------------------------------------------------------------ *
+ * Around a causal FMA layer: queries and keys before it, and the cache
+ * that answers token by token what the layer was trained on.
+ * ------------------------------------------------------------------ */
+
+/* A tensor [batch][heads][tokens][head_dim] of the plan's dtype anywhere in
+ * memory: element strides of the first three axes, channels adjacent.  data
+ * 16-byte aligned; strides of axes longer than 1 non-negative multiples of 16
+ * bytes (FMA_ERR_ALIGN, FMA_ERR_SHAPE).  Inputs may repeat rows (stride 0),
+ * outputs may not (FMA_ERR_ARG).  The rows of a packed projection
+ * [batch][tokens][all heads][d] are such a tensor, so is [batch][heads][tokens][d]. */
+typedef struct {
+    void *data;
+    int64_t batch_stride, head_stride, token_stride;
+} fma_view_t;
+
+typedef struct fma_qk_plan_s *fma_qk_plan_t;   /* opaque, host-side, immutable */
+
+/* Norm and rotation of queries and keys:
+ *   z = gamma * x / sqrt(mean(x^2) + eps)     over the channels of one head
+ *   pair (a, b) of z -> (a cos t - b sin t, a sin t + b cos t)
+ * for the first rotary_dim channels; t = position * inv_freq[pair].  With axes
+ * = 2 (token maps) the first half of those channels turns by the row, the
+ * second by the column.  Within an axis' channels the pairs are (i, i + half),
+ * or with `interleaved` (2i, 2i + 1). */
+typedef struct {
+    int32_t struct_size;      /* sizeof(fma_qk_desc_t) */
+    int32_t dtype;            /* fma_dtype_t */
+    int32_t heads;            /* query heads >= 1 */
+    int32_t kv_heads;         /* key / value heads >= 1, a divisor of heads */
+    int32_t head_dim;         /* 32, 64 or 128 */
+    int32_t rotary_dim;       /* 0 .. head_dim, a multiple of 16 * axes */
+    int32_t axes;             /* 1 or 2 */
+    int32_t side;             /* axes 2: the map's columns, for calls without positions */
+    int32_t interleaved;      /* 0 or 1 */
+    int32_t repeat_kv;        /* 1: keys and values leave once per query head (fma_forward_* takes
+                                 as many key as query heads); the backward adds their gradients */
+    float eps;                /* >= 0 */
+    double base;              /* inv_freq[i] = base^(-i / half); > 0 */
+} fma_qk_desc_t;
+
+/* Validate `desc` and build a plan (host memory only).  inv_freq: rotary_dim /
+ * (2 axes) rates in radians per position, on the host, copied; NULL takes
+ * them from `base`. */
+fma_status_t fma_qk_plan(const fma_qk_desc_t *desc, const double *inv_freq, fma_qk_plan_t *out_plan);
+
+/* Release a plan.  NULL is a no-op. */
+fma_status_t fma_qk_destroy(fma_qk_plan_t plan);
+
+/* q, k, v (heads, kv_heads, kv_heads) -> q_out, k_out, v_out (heads; kv_heads,
+ * or heads with repeat_kv) in one pass; v is copied.  v and v_out may be NULL
+ * together.
+ *   gamma_q, gamma_k : fp32 device [head_dim]; NULL = ones
+ *   positions : int32 device [batch][tokens][axes], any values; NULL = the
+ *               token's index (axes 2: index / side, index % side)
+ * Angles are formed in fp64 turns, so far positions keep their accuracy.
+ * batch * tokens must stay below 2^28, less than 16385 heads (FMA_ERR_SHAPE).  An output may be its
+ * own input's view (in place; not with repeat_kv over shared heads); otherwise
+ * outputs must not overlap inputs or each other (the heads of one packed
+ * projection do not). */
+fma_status_t fma_qk_norm_rope(fma_qk_plan_t plan, int32_t batch, int64_t tokens,
+                              const fma_view_t *q, const fma_view_t *k, const fma_view_t *v,
+                              const float *gamma_q, const float *gamma_k, const int32_t *positions,
+                              const fma_view_t *q_out, const fma_view_t *k_out, const fma_view_t *v_out,
+                              void *stream);
+
+/* Device workspace of the backward (partial sums of the gammas' gradients). */
+fma_status_t fma_qk_backward_workspace_size(fma_qk_plan_t plan, int32_t batch, int64_t tokens, size_t *bytes);
+
+/* Gradients of fma_qk_norm_rope: from the inputs q, k and the gradients g_q,
+ * g_k, g_v of its outputs (shapes of the outputs) to dq, dk, dv (shapes of the
+ * inputs) and dgamma_q, dgamma_k (fp32 [head_dim], overwritten; NULL = not
+ * wanted).  g_v and dv may be NULL together.  dq, dk, dv may be the views of
+ * g_q, g_k, g_v (not with repeat_kv over shared heads) or of q, k; otherwise
+ * nothing may overlap.  Deterministic (no atomics). */
+fma_status_t fma_qk_norm_rope_backward(fma_qk_plan_t plan, int32_t batch, int64_t tokens,
+                                       const fma_view_t *q, const fma_view_t *k,
+                                       const float *gamma_q, const float *gamma_k, const int32_t *positions,
+                                       const fma_view_t *g_q, const fma_view_t *g_k, const fma_view_t *g_v,
+                                       const fma_view_t *dq, const fma_view_t *dk, const fma_view_t *dv,
+                                       float *dgamma_q, float *dgamma_k,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *fma_last_error(void);
 

@@ -69,6 +69,32 @@ class fma_desc_t(ctypes.Structure):
     ]
 
 
+class fma_view_t(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("batch_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+    ]
+
+
+class fma_qk_desc_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("axes", ctypes.c_int32),
+        ("side", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("repeat_kv", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("base", ctypes.c_double),
+    ]
+
+
 _lib = None
 
 
@@ -100,7 +126,15 @@ def library() -> ctypes.CDLL:
     lib.fma_forward_static.argtypes = [vp] * 8
     lib.fma_stream_reference.argtypes = [vp, ctypes.c_size_t, vp, ctypes.c_size_t, i32, vp]
     lib.fma_plan_params.argtypes = [vp, ctypes.POINTER(i64), i32, ctypes.POINTER(i32)]
-    for name in ("fma_plan", "fma_destroy", "fma_workspace_size", "fma_weights_len", "fma_coarse_rows",
+    view = ctypes.POINTER(fma_view_t)
+    lib.fma_qk_plan.argtypes = [ctypes.POINTER(fma_qk_desc_t), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(vp)]
+    lib.fma_qk_destroy.argtypes = [vp]
+    lib.fma_qk_norm_rope.argtypes = [vp, i32, i64, view, view, view, vp, vp, vp, view, view, view, vp]
+    lib.fma_qk_backward_workspace_size.argtypes = [vp, i32, i64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.fma_qk_norm_rope_backward.argtypes = [vp, i32, i64, view, view, vp, vp, vp] + [view] * 6 + [
+        vp, vp, vp, ctypes.c_size_t, vp]
+    for name in ("fma_qk_plan", "fma_qk_destroy", "fma_qk_norm_rope", "fma_qk_backward_workspace_size",
+                 "fma_qk_norm_rope_backward", "fma_plan", "fma_destroy", "fma_workspace_size", "fma_weights_len", "fma_coarse_rows",
                  "fma_num_levels", "fma_forward_1d", "fma_forward_2d", "fma_coarsen", "fma_attend",
                  "fma_interaction_lists", "fma_dense_reference", "fma_backward_workspace_size",
                  "fma_backward", "fma_backward_linear", "fma_forward_linear", "fma_forward_static",
@@ -260,6 +294,37 @@ def fma_backward_linear(plan, q, k, v, wk, wv, wq, out, dout, dq, dk, dv, dwk, d
                                          _ptr(dwv), _ptr(dwq), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
+def fma_qk_plan(desc: fma_qk_desc_t, inv_freq=None) -> int:
+    h = ctypes.c_void_p()
+    rates = None if inv_freq is None else (ctypes.c_double * len(inv_freq))(*inv_freq)
+    _check(library().fma_qk_plan(ctypes.byref(desc), rates, ctypes.byref(h)))
+    return h.value
+
+
+def fma_qk_destroy(plan: int) -> None:
+    _check(library().fma_qk_destroy(plan))
+
+
+def fma_qk_norm_rope(plan, batch, tokens, q, k, v, gamma_q, gamma_k, positions, q_out, k_out, v_out, stream=None):
+    """q, k, v, q_out, k_out, v_out: fma_view_t (v, v_out may be None)."""
+    _check(library().fma_qk_norm_rope(plan, batch, tokens, q, k, v, _ptr(gamma_q), _ptr(gamma_k), _ptr(positions),
+                                      q_out, k_out, v_out, _stream(stream)))
+
+
+def fma_qk_backward_workspace_size(plan: int, batch: int, tokens: int) -> int:
+    x = ctypes.c_size_t()
+    _check(library().fma_qk_backward_workspace_size(plan, batch, tokens, ctypes.byref(x)))
+    return x.value
+
+
+def fma_qk_norm_rope_backward(plan, batch, tokens, q, k, gamma_q, gamma_k, positions, g_q, g_k, g_v, dq, dk, dv,
+                              dgamma_q, dgamma_k, workspace, workspace_bytes, stream=None):
+    """q, k, g_q, g_k, g_v, dq, dk, dv: fma_view_t (g_v, dv may be None)."""
+    _check(library().fma_qk_norm_rope_backward(plan, batch, tokens, q, k, _ptr(gamma_q), _ptr(gamma_k),
+                                               _ptr(positions), g_q, g_k, g_v, dq, dk, dv, _ptr(dgamma_q),
+                                               _ptr(dgamma_k), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
 def fma_last_error() -> str:
     return library().fma_last_error().decode()
 
@@ -414,3 +479,172 @@ class FMA:
             out = torch.empty_like(q)
         fma_dense_reference(self.handle, q, k, v, out, stream)
         return out
+
+
+# ---------------------------------------------------------------- strided calls
+def _dtype_code(dtype):
+    if dtype not in _DTYPES:
+        _refuse(FMA_ERR_ARG, "dtype %s is neither float32 nor bfloat16", dtype)
+    return _DTYPES[dtype]
+
+
+def _refuse(status, message, *args):
+    raise FmaError(status, message % args)
+
+
+def _view(t, name, shape, axes, dtype, device):
+    """fma_view_t of a tensor whose axes (batch, heads, tokens) are `axes`."""
+    if t.shape != shape:
+        _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), tuple(shape))
+    if t.dtype != dtype or t.device != device:
+        _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, dtype, device)
+    s = t.stride()
+    if s[3] != 1:
+        _refuse(FMA_ERR_SHAPE, "the channels of %s are not adjacent", name)
+    return fma_view_t(t.data_ptr(), s[axes[0]], s[axes[1]], s[axes[2]])
+
+
+_TOKEN_MAJOR, _HEAD_MAJOR = (0, 2, 1), (0, 1, 2)   # [batch, tokens, heads, d], [batch, heads, tokens, d]
+
+
+def _plain(t, name, shape, dtype, device):
+    """A dense side input (None passes)."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device:
+        _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, dtype, device)
+    if t.shape != shape:
+        _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), tuple(shape))
+    if not t.is_contiguous():
+        _refuse(FMA_ERR_SHAPE, "%s is not contiguous", name)
+
+
+class _Launch:
+    """Makes `device` current for a call, and `stream`, if the caller names
+    one, the stream that the call's allocations belong to."""
+
+    def __init__(self, device, stream):
+        if device.type != "cuda":
+            _refuse(FMA_ERR_ARG, "tensors are on %s, expected a GPU", device)
+        self.entered = []
+        if device.index != torch.cuda.current_device():
+            self.entered.append(torch.cuda.device(device))
+        if stream is not None:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=device)
+            if stream.device != device:
+                _refuse(FMA_ERR_ARG, "the stream belongs to %s, the tensors are on %s", stream.device, device)
+            self.entered.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.entered:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.entered):
+            c.__exit__(*exc)
+
+
+class QKNormRope:
+    """Per-head RMS norm and rotation of queries and keys, and the layout that
+    ``FMA.forward`` reads, in one pass over a projection's output; its
+    backward pass goes from ``FMA.backward``'s gradients to the projection's::
+
+        op = QKNormRope(heads=16, kv_heads=4, repeat_kv=True, dtype=torch.bfloat16)
+        q, k, v = op.forward(q, k, v, gamma_q, gamma_k)      # [B, n, heads, d] -> [B, heads, n, d]
+        dq, dk, dv, dgamma_q, dgamma_k = op.backward(q_in, k_in, gamma_q, gamma_k, gq, gk, gv)
+
+    axes = 2 rotates a map's tokens by row and column; inv_freq (a sequence of
+    rates per position) replaces base ** (-i / half).  repeat_kv gives keys and
+    values out once per query head.
+    """
+
+    def __init__(self, heads, kv_heads=None, head_dim=HEAD_DIM, dtype=torch.bfloat16, rotary_dim=None,
+                 base=10000.0, eps=1e-6, axes=1, side=0, interleaved=False, repeat_kv=False, inv_freq=None):
+        kv_heads = heads if kv_heads is None else kv_heads
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        if inv_freq is not None and len(inv_freq) != rotary_dim // (2 * max(axes, 1)):
+            _refuse(FMA_ERR_SHAPE, "inv_freq has %d rates, expected %d", len(inv_freq), rotary_dim // (2 * max(axes, 1)))
+        self.desc = fma_qk_desc_t(ctypes.sizeof(fma_qk_desc_t), _dtype_code(dtype), heads, kv_heads, head_dim, rotary_dim,
+                                  axes, side, int(bool(interleaved)), int(bool(repeat_kv)), eps, base)
+        self.handle = fma_qk_plan(self.desc, inv_freq)
+        self.heads, self.kv_heads, self.head_dim, self.dtype, self.axes = heads, kv_heads, head_dim, dtype, axes
+        self.kv_out = heads if repeat_kv else kv_heads
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h:
+            try:
+                library().fma_qk_destroy(h)
+            except Exception:
+                pass
+            self.handle = None
+
+    def _side(self, dev, gamma_q, gamma_k, positions, B, n):
+        d = self.head_dim
+        _plain(gamma_q, "gamma_q", (d,), torch.float32, dev)
+        _plain(gamma_k, "gamma_k", (d,), torch.float32, dev)
+        if positions is not None and positions.dim() == 2 and self.axes == 1:
+            positions = positions[..., None]
+        _plain(positions, "positions", (B, n, self.axes), torch.int32, dev)
+        return positions
+
+    def forward(self, q, k, v=None, gamma_q=None, gamma_k=None, positions=None, q_out=None, k_out=None, v_out=None,
+                stream=None):
+        """q [B, n, heads, d], k and v [B, n, kv_heads, d], any strides with
+        adjacent channels -> q_out, k_out, v_out [B, heads, n, d] (new dense
+        tensors, or the ones given, of any strides; token-major ones as
+        ``t.transpose(1, 2)``).  positions: int32 [B, n] or [B, n, axes]."""
+        if q.dim() != 4:
+            _refuse(FMA_ERR_SHAPE, "q has %d axes, expected [B, n, heads, d]", q.dim())
+        B, n, dev, d = q.shape[0], q.shape[1], q.device, self.head_dim
+        with _Launch(dev, stream):
+            positions = self._side(dev, gamma_q, gamma_k, positions, B, n)
+            if q_out is None:
+                q_out = torch.empty((B, self.heads, n, d), dtype=self.dtype, device=dev)
+            if k_out is None:
+                k_out = torch.empty((B, self.kv_out, n, d), dtype=self.dtype, device=dev)
+            if v is not None and v_out is None:
+                v_out = torch.empty((B, self.kv_out, n, d), dtype=self.dtype, device=dev)
+            a = (self.dtype, dev)
+            kvs, outs = (B, n, self.kv_heads, d), (B, self.kv_out, n, d)
+            fma_qk_norm_rope(
+                self.handle, B, n, _view(q, "q", (B, n, self.heads, d), _TOKEN_MAJOR, *a),
+                _view(k, "k", kvs, _TOKEN_MAJOR, *a), None if v is None else _view(v, "v", kvs, _TOKEN_MAJOR, *a),
+                gamma_q, gamma_k, positions, _view(q_out, "q_out", (B, self.heads, n, d), _HEAD_MAJOR, *a),
+                _view(k_out, "k_out", outs, _HEAD_MAJOR, *a),
+                None if v_out is None else _view(v_out, "v_out", outs, _HEAD_MAJOR, *a))
+        return q_out, k_out, v_out
+
+    def backward(self, q, k, gamma_q, gamma_k, g_q, g_k, g_v=None, positions=None, dq=None, dk=None, dv=None,
+                 workspace=None, stream=None):
+        """(dq, dk, dv, dgamma_q, dgamma_k) from the forward's q, k and the
+        gradients of its outputs; dq, dk, dv [B, n, heads, d] (new, or the
+        tensors given, of any strides: the heads of one packed gradient).  A
+        gamma of None has no gradient."""
+        if q.dim() != 4:
+            _refuse(FMA_ERR_SHAPE, "q has %d axes, expected [B, n, heads, d]", q.dim())
+        B, n, dev, d = q.shape[0], q.shape[1], q.device, self.head_dim
+        kvs, outs = (B, n, self.kv_heads, d), (B, self.kv_out, n, d)
+        with _Launch(dev, stream):
+            positions = self._side(dev, gamma_q, gamma_k, positions, B, n)
+            new = lambda *s: torch.empty(s, dtype=self.dtype, device=dev)  # noqa: E731
+            dq = new(B, n, self.heads, d) if dq is None else dq
+            dk = new(*kvs) if dk is None else dk
+            if g_v is not None and dv is None:
+                dv = new(*kvs)
+            dgq = None if gamma_q is None else torch.empty_like(gamma_q)
+            dgk = None if gamma_k is None else torch.empty_like(gamma_k)
+            need = fma_qk_backward_workspace_size(self.handle, B, n)
+            if workspace is None:
+                workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+            a = (self.dtype, dev)
+            fma_qk_norm_rope_backward(
+                self.handle, B, n, _view(q, "q", (B, n, self.heads, d), _TOKEN_MAJOR, *a),
+                _view(k, "k", kvs, _TOKEN_MAJOR, *a), gamma_q, gamma_k, positions,
+                _view(g_q, "g_q", (B, self.heads, n, d), _HEAD_MAJOR, *a), _view(g_k, "g_k", outs, _HEAD_MAJOR, *a),
+                None if g_v is None else _view(g_v, "g_v", outs, _HEAD_MAJOR, *a),
+                _view(dq, "dq", (B, n, self.heads, d), _TOKEN_MAJOR, *a), _view(dk, "dk", kvs, _TOKEN_MAJOR, *a),
+                None if dv is None else _view(dv, "dv", kvs, _TOKEN_MAJOR, *a), dgq, dgk, workspace,
+                workspace.numel() * workspace.element_size())
+        return dq, dk, dv, dgq, dgk

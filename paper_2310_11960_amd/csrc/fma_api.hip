@@ -10,6 +10,7 @@
 #include <mutex>
 #include <new>
 
+#include "api_status.hpp"
 #include "fma.h"
 #include "fma_kernels.hpp"
 
@@ -115,6 +116,20 @@ fma_status_t ok()
     g_err[0] = 0;
     return FMA_OK;
 }
+
+}  // namespace
+
+fma_status_t fma_dev::set_status(fma_status_t st, const char *fmt, ...)
+{
+    if (!fmt) return ok();
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+namespace {
 
 int levels_for(long long ratio)
 {
