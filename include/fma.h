@@ -410,6 +410,103 @@ fma_status_t fma_qk_norm_rope_backward(fma_qk_plan_t plan, int32_t batch, int64_
                                        float *dgamma_q, float *dgamma_k,
                                        void *workspace, size_t workspace_bytes, void *stream);
 
+typedef struct fma_cache_plan_s *fma_cache_plan_t;   /* opaque, host-side, immutable */
+
+/* Paged cache of a causal 1D FMA layer under the joint normalisation, for
+ * prompts in pieces and for single tokens.  What a query attends to depends
+ * only on tokens up to its own, so the cached form gives what fma_forward_1d
+ * gives for the whole sequence, at any length.
+ *
+ * A page holds one base block's keys (or values), kv_heads x block x head_dim.
+ * A summary page holds, for one complete block b, the running sums of every
+ * coarse set e = (level l, basis s) over the block's level-l group up to the
+ * end of b:
+ *   S_e(b) = sum over tokens j of the group, j < (b + 1) * block, of
+ *            pi_e[j - start(G)] * k_j   (values likewise),
+ * so the coarse key of a group is S_e of its last block.  Nothing else is kept:
+ *   - tokens of complete blocks can be shared between sequences by sharing
+ *     pages and summary pages, and a sequence can go back to any length whose
+ *     pages it still has by naming that length;
+ *   - the page of block b is no longer read once the sequence is past block
+ *     b + 1; the summary page of block b is read while b is the block before
+ *     the newest, and at level l (from 1) while b is the last block of one of
+ *     the two groups before the newest query's parent pair of groups and after. */
+typedef struct {
+    int32_t struct_size;      /* sizeof(fma_cache_desc_t) */
+    int32_t dtype;            /* fma_dtype_t */
+    int32_t heads;            /* query heads >= 1 */
+    int32_t kv_heads;         /* key / value heads >= 1, a divisor of heads */
+    int32_t head_dim;         /* 32, 64 or 128 */
+    int32_t block;            /* r: 16, 32 or a multiple of 64 up to 256 */
+    int64_t max_seq_len;      /* longest sequence >= 1; fixes the levels: those of fma_plan
+                                 for ceil(max_seq_len / r) blocks */
+    int32_t rank;             /* p >= 1 basis vectors per level; 0 selects 1 */
+    int32_t weights_per_head; /* 1: weights are [kv_heads][wlen]; 0: one [wlen] set */
+    int32_t norm;             /* FMA_NORM_JOINT (per-level: FMA_ERR_UNSUPPORTED) */
+    float softmax_scale;      /* tau, any finite value; 0 selects 1/sqrt(head_dim) */
+} fma_cache_desc_t;
+
+/* Validate `desc` and build a plan (host memory only). */
+fma_status_t fma_cache_plan(const fma_cache_desc_t *desc, fma_cache_plan_t *out_plan);
+
+/* Release a plan.  NULL is a no-op. */
+fma_status_t fma_cache_destroy(fma_cache_plan_t plan);
+
+/* Coarse sets (levels * rank), fp32 weights per head for each of pi^k and
+ * pi^v (layout of fma_weights_len), and blocks of the longest sequence. */
+fma_status_t fma_cache_sizes(fma_cache_plan_t plan, int32_t *sets, int64_t *weights_len, int64_t *blocks);
+
+/* The caller's storage and one batch of sequences.  Device arrays unless said
+ * otherwise. */
+typedef struct {
+    void *k_pages, *v_pages;        /* [num_pages][kv_heads][block][head_dim], plan dtype, 16-byte aligned */
+    float *summaries;               /* [num_summaries][kv_heads][2 (k, v)][sets][head_dim], 16-byte
+                                       aligned (NULL when sets == 0) */
+    int64_t num_pages, num_summaries;   /* host values */
+    const int32_t *page_table;      /* [sequences][table_stride]: page of every block */
+    const int32_t *summary_table;   /* [sequences][table_stride]: its summary page (NULL when sets == 0) */
+    int64_t table_stride;           /* host value: entries per sequence */
+    const int32_t *cu_tokens;       /* [sequences + 1]: sequence i's new tokens are rows
+                                       cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's tensors */
+    const int32_t *start;           /* [sequences]: tokens that the sequence already has */
+    int32_t sequences;              /* host value */
+    int32_t max_chunk;              /* host value: no sequence has more new tokens */
+    int64_t rows;                   /* host value: rows of the call's tensors */
+} fma_cache_batch_t;
+
+/* Rules of the three calls below.
+ *   - Tensors are views of batch 1: q and out [heads] rows, k and v [kv_heads]
+ *     rows per token (batch_stride is not read).
+ *   - Lengths and tables live on the device and may change between replays of
+ *     a captured call; only host values shape the launch.
+ *   - A sequence whose entries do not fit (rows outside the tensors, more new
+ *     tokens than max_chunk, a length past max_seq_len or the table) is
+ *     skipped: nothing of it is read or written.  Rows of no sequence are
+ *     left as they were.
+ *   - A table entry outside the pool is a missing page: its tokens are neither
+ *     written nor seen by queries of other calls, its sums count as zero.  A row that sees
+ *     nothing is zero.
+ *   - Pages written by a call must not be shared by its sequences.
+ *   - Calls on one cache are ordered by the caller (one stream); they may be
+ *     repeated with the same result, no atomics. */
+
+/* New keys and values into the pages, and the summaries of the blocks that
+ * they complete.  wk, wv as in fma_forward_1d ([kv_heads][wlen] or [wlen];
+ * NULL when sets == 0). */
+fma_status_t fma_cache_append(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *k,
+                              const fma_view_t *v, const float *wk, const float *wv, void *stream);
+
+/* FMA attention of queries at positions start .. start + new tokens - 1, whose
+ * keys and values are in the cache already. */
+fma_status_t fma_cache_attend(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
+                              const fma_view_t *out, void *stream);
+
+/* fma_cache_append, then fma_cache_attend, in one launch where no sequence has
+ * more than `block` new tokens.  A row always sees its own token here. */
+fma_status_t fma_cache_step(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
+                            const fma_view_t *k, const fma_view_t *v, const float *wk, const float *wv,
+                            const fma_view_t *out, void *stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *fma_last_error(void);
 

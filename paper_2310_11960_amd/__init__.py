@@ -18,6 +18,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+from typing import NamedTuple
 
 import torch
 
@@ -95,6 +96,40 @@ class fma_qk_desc_t(ctypes.Structure):
     ]
 
 
+class fma_cache_desc_t(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("block", ctypes.c_int32),
+        ("max_seq_len", ctypes.c_int64),
+        ("rank", ctypes.c_int32),
+        ("weights_per_head", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+    ]
+
+
+class fma_cache_batch_t(ctypes.Structure):
+    _fields_ = [
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("summaries", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int64),
+        ("num_summaries", ctypes.c_int64),
+        ("page_table", ctypes.c_void_p),
+        ("summary_table", ctypes.c_void_p),
+        ("table_stride", ctypes.c_int64),
+        ("cu_tokens", ctypes.c_void_p),
+        ("start", ctypes.c_void_p),
+        ("sequences", ctypes.c_int32),
+        ("max_chunk", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+    ]
+
+
 _lib = None
 
 
@@ -133,7 +168,15 @@ def library() -> ctypes.CDLL:
     lib.fma_qk_backward_workspace_size.argtypes = [vp, i32, i64, ctypes.POINTER(ctypes.c_size_t)]
     lib.fma_qk_norm_rope_backward.argtypes = [vp, i32, i64, view, view, vp, vp, vp] + [view] * 6 + [
         vp, vp, vp, ctypes.c_size_t, vp]
-    for name in ("fma_qk_plan", "fma_qk_destroy", "fma_qk_norm_rope", "fma_qk_backward_workspace_size",
+    batch = ctypes.POINTER(fma_cache_batch_t)
+    lib.fma_cache_plan.argtypes = [ctypes.POINTER(fma_cache_desc_t), ctypes.POINTER(vp)]
+    lib.fma_cache_destroy.argtypes = [vp]
+    lib.fma_cache_sizes.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    lib.fma_cache_append.argtypes = [vp, batch, view, view, vp, vp, vp]
+    lib.fma_cache_attend.argtypes = [vp, batch, view, view, vp]
+    lib.fma_cache_step.argtypes = [vp, batch, view, view, view, vp, vp, view, vp]
+    for name in ("fma_cache_plan", "fma_cache_destroy", "fma_cache_sizes", "fma_cache_append", "fma_cache_attend",
+                 "fma_cache_step", "fma_qk_plan", "fma_qk_destroy", "fma_qk_norm_rope", "fma_qk_backward_workspace_size",
                  "fma_qk_norm_rope_backward", "fma_plan", "fma_destroy", "fma_workspace_size", "fma_weights_len", "fma_coarse_rows",
                  "fma_num_levels", "fma_forward_1d", "fma_forward_2d", "fma_coarsen", "fma_attend",
                  "fma_interaction_lists", "fma_dense_reference", "fma_backward_workspace_size",
@@ -323,6 +366,36 @@ def fma_qk_norm_rope_backward(plan, batch, tokens, q, k, gamma_q, gamma_k, posit
     _check(library().fma_qk_norm_rope_backward(plan, batch, tokens, q, k, _ptr(gamma_q), _ptr(gamma_k),
                                                _ptr(positions), g_q, g_k, g_v, dq, dk, dv, _ptr(dgamma_q),
                                                _ptr(dgamma_k), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def fma_cache_plan(desc: fma_cache_desc_t) -> int:
+    h = ctypes.c_void_p()
+    _check(library().fma_cache_plan(ctypes.byref(desc), ctypes.byref(h)))
+    return h.value
+
+
+def fma_cache_destroy(plan: int) -> None:
+    _check(library().fma_cache_destroy(plan))
+
+
+def fma_cache_sizes(plan: int) -> tuple[int, int, int]:
+    """(coarse sets, weights per head, blocks of the longest sequence)."""
+    sets, wlen, blocks = ctypes.c_int32(), ctypes.c_int64(), ctypes.c_int64()
+    _check(library().fma_cache_sizes(plan, ctypes.byref(sets), ctypes.byref(wlen), ctypes.byref(blocks)))
+    return sets.value, wlen.value, blocks.value
+
+
+def fma_cache_append(plan, batch, k, v, wk, wv, stream=None):
+    """batch: fma_cache_batch_t; k, v: fma_view_t."""
+    _check(library().fma_cache_append(plan, batch, k, v, _ptr(wk), _ptr(wv), _stream(stream)))
+
+
+def fma_cache_attend(plan, batch, q, out, stream=None):
+    _check(library().fma_cache_attend(plan, batch, q, out, _stream(stream)))
+
+
+def fma_cache_step(plan, batch, q, k, v, wk, wv, out, stream=None):
+    _check(library().fma_cache_step(plan, batch, q, k, v, _ptr(wk), _ptr(wv), out, _stream(stream)))
 
 
 def fma_last_error() -> str:
@@ -648,3 +721,141 @@ class QKNormRope:
                 None if dv is None else _view(dv, "dv", kvs, _TOKEN_MAJOR, *a), dgq, dgk, workspace,
                 workspace.numel() * workspace.element_size())
         return dq, dk, dv, dgq, dgk
+
+
+class CachePages(NamedTuple):
+    """Storage of a paged cache: k, v [pages, kv_heads, block, d]; summaries
+    fp32 [pages, kv_heads, 2, sets, d] (None without coarse sets)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    summaries: torch.Tensor | None = None
+
+
+class CacheBatch(NamedTuple):
+    """One call's sequences, int32 on the GPU: sequence i has start[i] tokens
+    and rows cu_tokens[i] .. cu_tokens[i + 1] - 1 of the call's tensors are its
+    next ones, at most max_chunk; page_table, summary_table [sequences,
+    blocks]: the pages of its blocks."""
+    cu_tokens: torch.Tensor
+    start: torch.Tensor
+    page_table: torch.Tensor
+    summary_table: torch.Tensor | None
+    max_chunk: int
+
+
+class FMACache:
+    """Paged cache of a causal FMA layer: prompts in pieces, single tokens, or
+    both in one ragged batch, with what ``FMA.forward`` gives for the whole
+    sequences (causal, joint normalisation)::
+
+        op = FMACache(heads=16, kv_heads=4, block=128, max_seq_len=65536, dtype=torch.bfloat16)
+        pages = op.new_pages(num_pages, num_summaries, "cuda")
+        op.append(k, v, wk, wv, pages, batch)             # k, v: [tokens, kv_heads, d]
+        out = op.step(q, k, v, wk, wv, pages, batch)      # appends and attends, q, out: [tokens, heads, d]
+    """
+
+    def __init__(self, heads, max_seq_len, kv_heads=None, head_dim=HEAD_DIM, block=64, dtype=torch.bfloat16, rank=1,
+                 weights_per_head=True, softmax_scale=0.0, norm=FMA_NORM_JOINT):
+        kv_heads = heads if kv_heads is None else kv_heads
+        self.desc = fma_cache_desc_t(ctypes.sizeof(fma_cache_desc_t), _dtype_code(dtype), heads, kv_heads, head_dim, block,
+                                     max_seq_len, rank, int(bool(weights_per_head)), norm, softmax_scale)
+        self.handle = fma_cache_plan(self.desc)
+        self.heads, self.kv_heads, self.head_dim, self.block, self.dtype = heads, kv_heads, head_dim, block, dtype
+        self.weights_per_head = bool(weights_per_head)
+        self.sets, self.weights_len, self.blocks = fma_cache_sizes(self.handle)
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h:
+            try:
+                library().fma_cache_destroy(h)
+            except Exception:
+                pass
+            self.handle = None
+
+    def new_pages(self, num_pages, num_summaries, device) -> CachePages:
+        page = (num_pages, self.kv_heads, self.block, self.head_dim)
+        sums = (num_summaries, self.kv_heads, 2, self.sets, self.head_dim)
+        return CachePages(torch.empty(page, dtype=self.dtype, device=device),
+                          torch.empty(page, dtype=self.dtype, device=device),
+                          torch.empty(sums, dtype=torch.float32, device=device) if self.sets else None)
+
+    # ---------------------------------------------------------- helpers
+    def _batch(self, pages, batch, rows, dev):
+        kp, vp, sums = pages
+        cu, start, table, stable, chunk = batch
+        S, i32 = start.shape[0], torch.int32
+        if kp.dim() != 4 or table.dim() != 2 or start.dim() != 1:
+            _refuse(FMA_ERR_SHAPE, "expected pages [n, kv_heads, block, d], tables [sequences, blocks], start [sequences]")
+        page = (kp.shape[0], self.kv_heads, self.block, self.head_dim)
+        _plain(kp, "k_pages", page, self.dtype, dev)
+        _plain(vp, "v_pages", page, self.dtype, dev)
+        _plain(cu, "cu_tokens", (S + 1,), i32, dev)
+        _plain(start, "start", (S,), i32, dev)
+        _plain(table, "page_table", (S, table.shape[1]), i32, dev)
+        nsum = 0
+        if self.sets:
+            if sums is None or stable is None:
+                _refuse(FMA_ERR_NULL, "the plan's coarse sets need summaries and a summary_table")
+            nsum = sums.shape[0]
+            _plain(sums, "summaries", (nsum, self.kv_heads, 2, self.sets, self.head_dim), torch.float32, dev)
+            _plain(stable, "summary_table", table.shape, i32, dev)
+        return fma_cache_batch_t(kp.data_ptr(), vp.data_ptr(), sums.data_ptr() if self.sets else None, kp.shape[0], nsum,
+                                 table.data_ptr(), stable.data_ptr() if self.sets else None, table.shape[1], cu.data_ptr(),
+                                 start.data_ptr(), S, chunk, rows)
+
+    def _rows(self, t, name, heads, rows, dev):
+        """fma_view_t of [tokens, heads, d]."""
+        if t.shape != (rows, heads, self.head_dim):
+            _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), (rows, heads, self.head_dim))
+        if t.dtype != self.dtype or t.device != dev:
+            _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, self.dtype, dev)
+        s = t.stride()
+        if s[2] != 1:
+            _refuse(FMA_ERR_SHAPE, "the channels of %s are not adjacent", name)
+        return fma_view_t(t.data_ptr(), 0, s[1], s[0])
+
+    def _weights(self, wk, wv, dev):
+        if not self.sets:
+            return None, None
+        shape = (self.kv_heads, self.weights_len) if self.weights_per_head else (self.weights_len,)
+        for name, w in (("wk", wk), ("wv", wv)):
+            if w is None:
+                _refuse(FMA_ERR_NULL, "%s is None", name)
+            _plain(w, name, shape, torch.float32, dev)
+        return wk, wv
+
+    # ---------------------------------------------------------- calls
+    def append(self, k, v, wk, wv, pages, batch, stream=None):
+        """New keys and values [tokens, kv_heads, d] (any strides, adjacent
+        channels) into the pages, and the summaries that they complete."""
+        rows, dev = k.shape[0], k.device
+        with _Launch(dev, stream):
+            wk, wv = self._weights(wk, wv, dev)
+            fma_cache_append(self.handle, self._batch(pages, batch, rows, dev),
+                             self._rows(k, "k", self.kv_heads, rows, dev), self._rows(v, "v", self.kv_heads, rows, dev),
+                             wk, wv)
+
+    def attend(self, q, pages, batch, out=None, stream=None):
+        """Attention of q [tokens, heads, d], whose keys and values are in the
+        cache, -> out (a new one is zero in rows of no sequence)."""
+        rows, dev = q.shape[0], q.device
+        with _Launch(dev, stream):
+            if out is None:
+                out = torch.zeros((rows, self.heads, self.head_dim), dtype=self.dtype, device=dev)
+            fma_cache_attend(self.handle, self._batch(pages, batch, rows, dev),
+                             self._rows(q, "q", self.heads, rows, dev), self._rows(out, "out", self.heads, rows, dev))
+        return out
+
+    def step(self, q, k, v, wk, wv, pages, batch, out=None, stream=None):
+        """append, then attend."""
+        rows, dev = q.shape[0], q.device
+        with _Launch(dev, stream):
+            wk, wv = self._weights(wk, wv, dev)
+            if out is None:
+                out = torch.zeros((rows, self.heads, self.head_dim), dtype=self.dtype, device=dev)
+            fma_cache_step(self.handle, self._batch(pages, batch, rows, dev),
+                           self._rows(q, "q", self.heads, rows, dev), self._rows(k, "k", self.kv_heads, rows, dev),
+                           self._rows(v, "v", self.kv_heads, rows, dev), wk, wv,
+                           self._rows(out, "out", self.heads, rows, dev))
+        return out

@@ -23,27 +23,12 @@
 //   lane's weights would pass 2^64.
 // Each row's 16-byte chunk c sits at chunk c ^ swzd(row).
 #include "attend_route.hpp"
+#include "lds_rows.hpp"
 #include "level_weights.hpp"
 
 namespace fma_dev {
 
 namespace {
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-// The swizzle keeps both the row reads of a 32x32 operand (lane = row) and the
-// transposing reads (four rows of two chunks per 16 lanes) on distinct banks;
-// rows are 64, 128 or 256 bytes.
-template <int D>
-__device__ inline int swzd(int row)
-{
-    const int s64 = (2 * (row & 3)) ^ ((row >> 2) & 1) ^ (2 * ((row >> 3) & 1));
-    if constexpr (D == 32) return (2 * ((row >> 1) & 1)) ^ ((row >> 2) & 1);
-    else if constexpr (D == 64) return s64;
-    else return s64 ^ (8 * (row & 1));
-}
 
 template <int D>
 constexpr int kTileRows = D == 128 ? 32 : 64;
@@ -57,7 +42,6 @@ struct GroupSmem {
 };
 
 __device__ inline float gexp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ inline int grow(int i, int hh) { return 8 * (i >> 2) + 4 * hh + (i & 3); }   // accumulator row
 
 // PL: printed per-level normalisation (levels inside a 32-slot piece).
 // SQ (scaled queries): c Q rounded to bf16, no running maximum and l from the

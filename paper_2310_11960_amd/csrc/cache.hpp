@@ -1,0 +1,149 @@
+// cache.hpp -- arguments, launchers and shared device code of the paged cache
+// (internal to the library).
+#pragma once
+
+#include "fma_device.hpp"
+
+namespace fma_dev {
+
+struct CacheArgs {
+    // rows of tokens: element strides of tokens and heads
+    const void *q, *k, *v;         // k == NULL: every key is in the pages
+    void *out;
+    int write;                     // the attention's launch puts k and v into the pages as well
+    long long qt, qh, kt, kh, vt, vh, ot, oh;
+    void *kp, *vp;                 // pages [npages][kv_heads][r][d]
+    float *sum;                    // summary pages [nsums][kv_heads][2][sets][d]
+    long long npages, nsums;
+    const int32_t *table, *stable; // [S][tstride]
+    long long tstride;
+    const int32_t *cu, *start;
+    const float *wk, *wv;
+    long long w_stride;            // floats between heads' weights (0 = shared)
+    int S, max_chunk, rows, limit; // limit: longest sequence that fits
+    int heads, kv_heads, group;    // group: query heads of a key head
+    int r, rank, levels, sets;
+    int head_dim, bf16;
+    float scale_log2;              // softmax scale * log2(e)
+};
+
+// How a launch's workgroups meet the sequences' tokens: tiles of tm positions
+// that do not cross base blocks, tpb of them per block.
+struct Tiling {
+    int tm, tpb;
+    int per_seq;   // > 0: workgroup u takes tile u % per_seq of sequence u / per_seq; 0: it searches
+    long long units;
+};
+
+hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
+hipError_t launch_cache_attend(const CacheArgs &a, hipStream_t st);   // a.write: a.max_chunk <= a.r
+
+__host__ __device__ inline int tile_of(const Tiling &t, int r, int pos) { return pos / r * t.tpb + pos % r / t.tm; }
+
+// Tiles of tm positions over chunks of at most a.max_chunk tokens.  A window of w
+// positions holds at most w tpb / r + 2 tile starts, so the rows tpb / r + 3 S
+// tiles bound any batch, and a tile has at least one row.  One tile range per
+// sequence, without a search, where that leaves at most twice as many idle
+// workgroups.
+inline Tiling make_tiling(const CacheArgs &a, int tm)
+{
+    Tiling t;
+    t.tm = tm < a.r ? tm : a.r;
+    t.tpb = (a.r + t.tm - 1) / t.tm;
+    const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
+    long long each = most * t.tpb / a.r + 3;
+    if (each > most) each = most;
+    long long bound = (long long)a.rows * t.tpb / a.r + 3LL * a.S;
+    if (bound > a.rows) bound = a.rows;
+    t.per_seq = each * a.S <= 2 * bound + 64 ? (int)each : 0;
+    t.units = t.per_seq ? each * a.S : bound;
+    return t;
+}
+
+// A workgroup's tile: positions [pos, pos + n) of sequence seq, the first in row
+// `row` of the call's tensors.
+struct Tile {
+    int seq, pos, n, row;
+    int start, end;     // tokens of the sequence before and after the call
+    int row0;           // row of its first new token
+};
+
+__device__ inline bool sequence_fits(const CacheArgs &a, int c0, int c1, int s)
+{
+    return c0 >= 0 && c1 > c0 && c1 <= a.rows && c1 - c0 <= a.max_chunk && s >= 0 && s <= a.limit - (c1 - c0);
+}
+
+__device__ inline bool find_tile(const CacheArgs &a, const Tiling &t, unsigned unit, Tile &x)
+{
+    int c0 = 0, s = 0, len = 0, idx = 0;
+    if (t.per_seq) {
+        x.seq = unit / (unsigned)t.per_seq;
+        idx = unit - x.seq * t.per_seq;
+        c0 = a.cu[x.seq];
+        const int c1 = a.cu[x.seq + 1];
+        s = a.start[x.seq];
+        if (!sequence_fits(a, c0, c1, s)) return false;
+        len = c1 - c0;
+        if (idx > tile_of(t, a.r, s + len - 1) - tile_of(t, a.r, s)) return false;
+    } else {
+        // 64 sequences at a time: their tile counts, a running sum over the
+        // lanes, and the first lane whose sum passes the unit
+        const int lane = threadIdx.x & 63;
+        int before = 0;
+        bool found = false;
+        for (int base = 0; base < a.S; base += 64) {
+            const int i = base + lane;
+            int n = 0, d0 = 0, d1 = 0, ds = 0;
+            if (i < a.S) {
+                d0 = a.cu[i];
+                d1 = a.cu[i + 1];
+                ds = a.start[i];
+                if (sequence_fits(a, d0, d1, ds)) n = tile_of(t, a.r, ds + d1 - d0 - 1) - tile_of(t, a.r, ds) + 1;
+            }
+            int sum = n;
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) {
+                const int y = __shfl_up(sum, k);
+                if (lane >= k) sum += y;
+            }
+            const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > (int)unit);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                x.seq = base + l;
+                idx = (int)unit - before - __shfl(sum - n, l);
+                c0 = __shfl(d0, l);
+                len = __shfl(d1, l) - c0;
+                s = __shfl(ds, l);
+                found = true;
+                break;
+            }
+            before += __shfl(sum, 63);
+        }
+        if (!found) return false;
+    }
+    const int tile = tile_of(t, a.r, s) + idx;
+    const int b = tile / t.tpb, lo = b * a.r + (tile - b * t.tpb) * t.tm;
+    int hi = lo + t.tm < (b + 1) * a.r ? lo + t.tm : (b + 1) * a.r;
+    if (hi > s + len) hi = s + len;
+    x.pos = lo > s ? lo : s;
+    x.n = hi - x.pos;
+    x.row = c0 + x.pos - s;
+    x.start = s;
+    x.end = s + len;
+    x.row0 = c0;
+    return true;
+}
+
+// page of block b (-1: missing)
+__device__ inline int page_of(const CacheArgs &a, int seq, int b)
+{
+    const int p = a.table[seq * a.tstride + b];
+    return p >= 0 && p < a.npages ? p : -1;
+}
+__device__ inline int summary_of(const CacheArgs &a, int seq, int b)
+{
+    const int p = a.stable[seq * a.tstride + b];
+    return p >= 0 && p < a.nsums ? p : -1;
+}
+
+}  // namespace fma_dev
