@@ -38,6 +38,16 @@ struct Tiling {
 hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
 hipError_t launch_cache_attend(const CacheArgs &a, hipStream_t st);   // a.write: a.max_chunk <= a.r
 
+hipError_t launch_cache_token(const CacheArgs &a, hipStream_t st);
+
+// Whether the attention runs on the vector ALU (cache_token.hip): at most four
+// query rows meet a key head's rows, too few for a 32-column matrix operand.
+inline bool token_rows(const CacheArgs &a)
+{
+    const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
+    return most * a.group <= 4;
+}
+
 __host__ __device__ inline int tile_of(const Tiling &t, int r, int pos) { return pos / r * t.tpb + pos % r / t.tm; }
 
 // Tiles of tm positions over chunks of at most a.max_chunk tokens.  A window of w

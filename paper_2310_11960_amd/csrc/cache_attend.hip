@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
     }
     if (a.write && g0 == 0 && a.sets && kend % a.r == 0) {
         __syncthreads();
-        summarize<BF16, D, NT>(a, x, h, b, page, true, sm.sum);
+        summarize<BF16, D, NT>(a, x, h, b, page, sm.sum);
     }
 }
 
@@ -258,6 +258,7 @@ hipError_t attend_d(const CacheArgs &a, hipStream_t st)
 hipError_t launch_cache_attend(const CacheArgs &a, hipStream_t st)
 {
     if (a.S == 0 || a.rows == 0 || a.max_chunk == 0) return hipSuccess;
+    if (token_rows(a)) return launch_cache_token(a, st);
     switch (a.head_dim) {
     case 32: return a.bf16 ? attend_d<true, 32>(a, st) : attend_d<false, 32>(a, st);
     case 64: return a.bf16 ? attend_d<true, 64>(a, st) : attend_d<false, 64>(a, st);

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "cache.hpp"
+#include "row_lanes.hpp"
 
 namespace fma_dev {
 
@@ -28,16 +29,7 @@ __device__ inline void *elem(void *p, long long off)
 template <bool BF16>
 __device__ inline void load8f(const void *p, float (&x)[8])
 {
-    if constexpr (BF16) {
-        const uint4 a = *static_cast<const uint4 *>(p);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i & 1 ? bf16hi_to_f32(w[i / 2]) : bf16lo_to_f32(w[i / 2]);
-    } else {
-        const float4 a = static_cast<const float4 *>(p)[0], b = static_cast<const float4 *>(p)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    }
+    floats<BF16>(load_raw<BF16>(p), x);
 }
 
 // A tile's new rows of key head h into their page (all in one block), NT threads.
@@ -66,73 +58,72 @@ struct SumSmem {
 
 // The summary of block b of key head h, complete with this call:
 //   S_e(b) = sum over its rows j of pi_e[b r mod s_l + j] x_j
-//            + (b starts a group of e's level ? 0 : S_e(b - 1)),
-// without the second term if !prior.  Rows from x.start on come from the
-// caller's tensors, the others from the block's page; d / 8 lanes hold a row.
-// fp32 throughout: sums over up to 2^15 blocks of a group are kept here.
+//            + (b starts a group of e's level ? 0 : S_e(b - 1)).
+// Rows from x.start on come from the caller's tensors, the others from the
+// block's page; d / 8 lanes hold a row, half of the waves the keys, the others
+// the values.  fp32 throughout: sums over up to 2^15 blocks of a group are kept.
 template <bool BF16, int D, int NT>
-__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, bool prior,
-                                 SumSmem<D, NT> &sm)
+__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, SumSmem<D, NT> &sm)
 {
-    constexpr int LPR = D / 8, SLOTS = NT / LPR;
+    constexpr int LPR = D / 8, NW = NT / 64, HT = NT / 2, SLOTS = HT / LPR;
     const int dst = summary_of(a, x.seq, b);
     if (dst < 0) return;
-    const int before = prior && b > 0 ? summary_of(a, x.seq, b - 1) : -1;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ch = 8 * (tid % LPR), slot = tid / LPR;
+    const int before = b > 0 ? summary_of(a, x.seq, b - 1) : -1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t = tid >= HT;
+    const int ch = 8 * (tid % LPR), slot = (tid - t * HT) / LPR;
+    const float *w = (t ? a.wv : a.wk) + h * a.w_stride;
     const long long row = (long long)a.sets * D;   // floats of one tensor's sums
-    for (int t = 0; t < 2; ++t) {
-        const float *w = (t ? a.wv : a.wk) + h * a.w_stride;
-        for (int e0 = 0; e0 < a.sets; e0 += kSumSets) {
-            float acc[kSumSets][8];
-            const float *we[kSumSets];
+    for (int e0 = 0; e0 < a.sets; e0 += kSumSets) {
+        float acc[kSumSets][8];
+        const float *we[kSumSets];
+#pragma unroll
+        for (int e = 0; e < kSumSets; ++e) {
+            const int l = (e0 + e) / a.rank, s = (e0 + e) - l * a.rank;
+            const long long size = (long long)a.r << l;
+            we[e] = w + a.rank * (size - a.r) + s * size + (long long)(b & ((1 << l) - 1)) * a.r;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[e][c] = 0.f;
+        }
+        for (int j = slot; j < a.r; j += SLOTS) {
+            const int pos = b * a.r + j;
+            float f[8];
+            if (pos >= x.start) {
+                const long long o = (long long)(x.row0 + pos - x.start) * (t ? a.vt : a.kt) + h * (t ? a.vh : a.kh);
+                load8f<BF16>(elem<BF16>(t ? a.v : a.k, o + ch), f);
+            } else if (page >= 0) {
+                load8f<BF16>(elem<BF16>(const_cast<const void *>(t ? a.vp : a.kp), page_row(a, page, h, j) + ch), f);
+            } else {
+                continue;
+            }
 #pragma unroll
             for (int e = 0; e < kSumSets; ++e) {
-                const int l = (e0 + e) / a.rank, s = (e0 + e) - l * a.rank;
-                const long long size = (long long)a.r << l;
-                we[e] = w + a.rank * (size - a.r) + s * size + (long long)(b & ((1 << l) - 1)) * a.r;
+                const float wj = e0 + e < a.sets ? we[e][j] : 0.f;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) acc[e][c] = 0.f;
+                for (int c = 0; c < 8; ++c) acc[e][c] = fmaf(wj, f[c], acc[e][c]);
             }
-            for (int j = slot; j < a.r; j += SLOTS) {
-                const int pos = b * a.r + j;
-                float f[8];
-                if (pos >= x.start) {
-                    const long long o = (long long)(x.row0 + pos - x.start) * (t ? a.vt : a.kt) + h * (t ? a.vh : a.kh);
-                    load8f<BF16>(elem<BF16>(t ? a.v : a.k, o + ch), f);
-                } else if (page >= 0) {
-                    load8f<BF16>(elem<BF16>(const_cast<const void *>(t ? a.vp : a.kp), page_row(a, page, h, j) + ch), f);
-                } else {
-                    continue;
-                }
+        }
 #pragma unroll
-                for (int e = 0; e < kSumSets; ++e) {
-                    const float wj = e0 + e < a.sets ? we[e][j] : 0.f;
+        for (int e = 0; e < kSumSets; ++e)
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) acc[e][c] = fmaf(wj, f[c], acc[e][c]);
-                }
+            for (int c = 0; c < 8; ++c) {
+#pragma unroll
+                for (int m = LPR; m < 64; m *= 2) acc[e][c] += __shfl_xor(acc[e][c], m);
+                if (lane < LPR) sm.part[wave][e][ch + c] = acc[e][c];
             }
-#pragma unroll
-            for (int e = 0; e < kSumSets; ++e)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-#pragma unroll
-                    for (int m = LPR; m < 64; m *= 2) acc[e][c] += __shfl_xor(acc[e][c], m);
-                    if (lane < LPR) sm.part[wave][e][ch + c] = acc[e][c];
-                }
-            __syncthreads();
-            for (int i = tid; i < kSumSets * D; i += NT) {
-                const int e = e0 + i / D, c = i % D;
-                if (e >= a.sets) break;
+        __syncthreads();
+        for (int i = tid; i < 2 * kSumSets * D; i += NT) {
+            const int kv = i / (kSumSets * D), e = i / D % kSumSets, c = i % D;
+            if (e0 + e < a.sets) {
                 float s = 0.f;
 #pragma unroll
-                for (int wv = 0; wv < NT / 64; ++wv) s += sm.part[wv][i / D][c];
-                const long long o = t * row + (long long)e * D + c;
-                if (before >= 0 && (b & ((1 << (e / a.rank)) - 1)))
+                for (int k = 0; k < NW / 2; ++k) s += sm.part[kv * (NW / 2) + k][e][c];
+                const long long o = kv * row + (long long)(e0 + e) * D + c;
+                if (before >= 0 && (b & ((1 << ((e0 + e) / a.rank)) - 1)))
                     s += a.sum[((long long)before * a.kv_heads + h) * 2 * row + o];
                 a.sum[((long long)dst * a.kv_heads + h) * 2 * row + o] = s;
             }
-            __syncthreads();
         }
+        __syncthreads();
     }
 }
 
