@@ -21,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libfma_mi355x.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 SOURCES = ["fma_api.hip", "coarsen.hip", "attend.hip", "attend_mfma.hip", "attend_group.hip", "lists.hip", "backward.hip", "backward_mfma.hip",
-           "stream_ref.hip", "qk_api.hip", "qk_norm_rope.hip", "cache_api.hip", "cache_append.hip", "cache_attend.hip", "cache_token.hip"]
+           "stream_ref.hip", "qk_api.hip", "qk_norm_rope.hip", "cache_api.hip", "cache_append.hip", "cache_attend.hip", "cache_token.hip", "cache_chunk.hip"]
 ARCH = "gfx950"
 
 

@@ -35,19 +35,6 @@ struct Tiling {
     long long units;
 };
 
-hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
-hipError_t launch_cache_attend(const CacheArgs &a, hipStream_t st);   // a.write: a.max_chunk <= a.r
-
-hipError_t launch_cache_token(const CacheArgs &a, hipStream_t st);
-
-// Whether the attention runs on the vector ALU (cache_token.hip): at most four
-// query rows meet a key head's rows, too few for a 32-column matrix operand.
-inline bool token_rows(const CacheArgs &a)
-{
-    const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
-    return most * a.group <= 4;
-}
-
 __host__ __device__ inline int tile_of(const Tiling &t, int r, int pos) { return pos / r * t.tpb + pos % r / t.tm; }
 
 // Tiles of tm positions over chunks of at most a.max_chunk tokens.  A window of w
@@ -70,6 +57,47 @@ inline Tiling make_tiling(const CacheArgs &a, int tm)
     return t;
 }
 
+// Which kernel attends:
+//   TOKENS  at most four query rows meet a key head's rows, too few for a
+//           32-column matrix operand: the vector ALU (cache_token.hip);
+//   KEYS    32 rows a workgroup, whose waves take different keys
+//           (cache_attend.hip): pieces whose rows with one key head fit one
+//           such tile, and calls of too few rows to fill the device with
+//   ROWS    128 rows a workgroup, whose waves take different rows and share the
+//           keys in LDS (cache_chunk.hip).
+// The first two put new tokens into the cache as well, where no chunk is longer
+// than a block (the far field of such a chunk has nothing of its own).
+enum CacheRoute { CACHE_TOKENS, CACHE_KEYS, CACHE_ROWS };
+
+// Query heads of a workgroup and workgroups per key head; the tile of CACHE_ROWS.
+struct ChunkShape {
+    int gs, split, tm;
+};
+inline ChunkShape chunk_shape(const CacheArgs &a)
+{
+    ChunkShape c;
+    c.split = (a.group + 31) / 32;
+    c.gs = (a.group + c.split - 1) / c.split;
+    int tpb = (a.r * c.gs + 127) / 128;   // equal tiles of at most 128 rows
+    while ((a.r + tpb - 1) / tpb * c.gs > 128) ++tpb;
+    c.tm = (a.r + tpb - 1) / tpb;
+    return c;
+}
+
+inline CacheRoute cache_route(const CacheArgs &a, int cus)
+{
+    const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
+    if (most * a.group <= 4) return CACHE_TOKENS;
+    const ChunkShape c = chunk_shape(a);
+    const long long groups = (long long)a.rows * c.gs / (c.tm * c.gs < 128 ? c.tm * c.gs : 128) * a.kv_heads * c.split;
+    return most * c.gs <= 32 || groups < cus ? CACHE_KEYS : CACHE_ROWS;
+}
+
+hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
+hipError_t launch_cache_token(const CacheArgs &a, hipStream_t st);
+hipError_t launch_cache_keys(const CacheArgs &a, const ChunkShape &c, hipStream_t st);
+hipError_t launch_cache_rows(const CacheArgs &a, const ChunkShape &c, hipStream_t st);
+
 // A workgroup's tile: positions [pos, pos + n) of sequence seq, the first in row
 // `row` of the call's tensors.
 struct Tile {
@@ -77,6 +105,12 @@ struct Tile {
     int start, end;     // tokens of the sequence before and after the call
     int row0;           // row of its first new token
 };
+
+// lengths and tables, which no kernel writes: scalar loads where the index is uniform
+__device__ inline int listed(const int32_t *p, long long i)
+{
+    return ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)p)[i];
+}
 
 __device__ inline bool sequence_fits(const CacheArgs &a, int c0, int c1, int s)
 {
@@ -89,9 +123,9 @@ __device__ inline bool find_tile(const CacheArgs &a, const Tiling &t, unsigned u
     if (t.per_seq) {
         x.seq = unit / (unsigned)t.per_seq;
         idx = unit - x.seq * t.per_seq;
-        c0 = a.cu[x.seq];
-        const int c1 = a.cu[x.seq + 1];
-        s = a.start[x.seq];
+        c0 = listed(a.cu, x.seq);
+        const int c1 = listed(a.cu, x.seq + 1);
+        s = listed(a.start, x.seq);
         if (!sequence_fits(a, c0, c1, s)) return false;
         len = c1 - c0;
         if (idx > tile_of(t, a.r, s + len - 1) - tile_of(t, a.r, s)) return false;
@@ -147,12 +181,12 @@ __device__ inline bool find_tile(const CacheArgs &a, const Tiling &t, unsigned u
 // page of block b (-1: missing)
 __device__ inline int page_of(const CacheArgs &a, int seq, int b)
 {
-    const int p = a.table[seq * a.tstride + b];
+    const int p = listed(a.table, seq * a.tstride + b);
     return p >= 0 && p < a.npages ? p : -1;
 }
 __device__ inline int summary_of(const CacheArgs &a, int seq, int b)
 {
-    const int p = a.stable[seq * a.tstride + b];
+    const int p = listed(a.stable, seq * a.tstride + b);
     return p >= 0 && p < a.nsums ? p : -1;
 }
 

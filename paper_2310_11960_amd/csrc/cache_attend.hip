@@ -15,7 +15,6 @@
 // for the second product (V's type); far rows, kept in fp32, to bf16 as the
 // dense path keeps them; maxima, sums and O are fp32.
 #include "cache_device.hpp"
-#include "lds_rows.hpp"
 #include "wave_ops.hpp"
 
 namespace fma_dev {
@@ -27,7 +26,7 @@ struct AttendSmem {
     union {
         __attribute__((aligned(16))) char v[NW][32 * D * (BF16 ? 2 : 4)];
         float o[NW][32][33];
-        SumSmem<D, 64 * NW> sum;
+        SumSmem<BF16, D, NW> sum;
     };
     float m[NW][32], l[NW][32];
 };
@@ -237,32 +236,30 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
         }
     }
     if (a.write && g0 == 0 && a.sets && kend % a.r == 0) {
+        const int dst = summary_of(a, x.seq, b), before = b > 0 ? summary_of(a, x.seq, b - 1) : -1;
         __syncthreads();
-        summarize<BF16, D, NT>(a, x, h, b, page, sm.sum);
+        if (dst >= 0) summarize<BF16, D, NW>(a, x, h, b, page, dst, before, sm.sum);
     }
 }
 
 template <bool BF16, int D>
-hipError_t attend_d(const CacheArgs &a, hipStream_t st)
+hipError_t attend_d(const CacheArgs &a, const ChunkShape &c, hipStream_t st)
 {
     constexpr int NW = BF16 ? 8 : 4;
-    const int split = (a.group + 31) / 32, gs = (a.group + split - 1) / split;
-    const Tiling t = make_tiling(a, 32 / gs);
-    hipLaunchKernelGGL((cache_attend_kernel<BF16, D, NW>), dim3((unsigned)t.units, a.kv_heads * split), dim3(64 * NW), 0,
-                       st, a, t, split, gs);
+    const Tiling t = make_tiling(a, 32 / c.gs);
+    hipLaunchKernelGGL((cache_attend_kernel<BF16, D, NW>), dim3((unsigned)t.units, a.kv_heads * c.split), dim3(64 * NW), 0,
+                       st, a, t, c.split, c.gs);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cache_attend(const CacheArgs &a, hipStream_t st)
+hipError_t launch_cache_keys(const CacheArgs &a, const ChunkShape &c, hipStream_t st)
 {
-    if (a.S == 0 || a.rows == 0 || a.max_chunk == 0) return hipSuccess;
-    if (token_rows(a)) return launch_cache_token(a, st);
     switch (a.head_dim) {
-    case 32: return a.bf16 ? attend_d<true, 32>(a, st) : attend_d<false, 32>(a, st);
-    case 64: return a.bf16 ? attend_d<true, 64>(a, st) : attend_d<false, 64>(a, st);
-    case 128: return a.bf16 ? attend_d<true, 128>(a, st) : attend_d<false, 128>(a, st);
+    case 32: return a.bf16 ? attend_d<true, 32>(a, c, st) : attend_d<false, 32>(a, c, st);
+    case 64: return a.bf16 ? attend_d<true, 64>(a, c, st) : attend_d<false, 64>(a, c, st);
+    case 128: return a.bf16 ? attend_d<true, 128>(a, c, st) : attend_d<false, 128>(a, c, st);
     default: return hipErrorInvalidValue;
     }
 }

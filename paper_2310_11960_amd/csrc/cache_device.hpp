@@ -3,6 +3,7 @@
 #pragma once
 
 #include "cache.hpp"
+#include "lds_rows.hpp"
 #include "row_lanes.hpp"
 
 namespace fma_dev {
@@ -32,6 +33,35 @@ __device__ inline void load8f(const void *p, float (&x)[8])
     floats<BF16>(load_raw<BF16>(p), x);
 }
 
+// The far field of queries in block b: level by level group q - 2 and (odd q)
+// group q - 3, each with all bases; groups that a finer level covers and
+// empty levels take no place in the list.
+struct FarList {
+    int b, levels, n;
+    __device__ FarList(const CacheArgs &a, int b_)
+    {
+        const int lq = b_ >= 2 ? 31 - __builtin_clz((unsigned)b_) : 0;
+        b = b_;
+        levels = lq < a.levels ? lq : a.levels;
+        n = a.rank * (levels + __popc(b & ((1 << levels) - 1)));
+    }
+    // key row of source i (the value row is sets * D floats on); NULL if its page is missing
+    __device__ const float *row(const CacheArgs &a, int seq, int h, int i) const
+    {
+        if (i >= n) return nullptr;
+        int lv = 0, c = a.rank << (b & 1);
+        while (i >= c) {
+            i -= c;
+            ++lv;
+            c = a.rank << (b >> lv & 1);
+        }
+        const int two = i >= a.rank, g = (b >> lv) - 2 - two;
+        const int sp = summary_of(a, seq, ((g + 1) << lv) - 1);
+        if (sp < 0) return nullptr;
+        return a.sum + (((long long)sp * a.kv_heads + h) * 2 * a.sets + lv * a.rank + i - two * a.rank) * a.head_dim;
+    }
+};
+
 // A tile's new rows of key head h into their page (all in one block), NT threads.
 template <bool BF16, int D, int NT>
 __device__ inline void copy_rows(const CacheArgs &a, const Tile &x, int h, int page)
@@ -49,78 +79,202 @@ __device__ inline void copy_rows(const CacheArgs &a, const Tile &x, int h, int p
     }
 }
 
-constexpr int kSumSets = 4;   // sets that one walk over a block's rows adds up
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // the caller's weights
 
-template <int D, int NT>
-struct SumSmem {
-    float part[NT / 64][kSumSets][D];
+// One wave's share of a block's sums: the block's rows (keys or values of head
+// h), 32 at a time, against the weights of sets s0 .. s0 + 31,
+//   o[db] += X^T W^T      (rows: channels 32 db .., columns: sets),
+// on the matrix cores.  fp32 weights meet bf16 rows exactly: each weight is
+// split into three bf16 terms (8 + 8 + 8 bits), so the sums keep fp32 accuracy.
+template <bool BF16, int D>
+struct BlockRows {
+    static constexpr int LPR = D / 8, RPL = 64 / LPR, NL = 32 / RPL, ND = D / 32;   // rows of a load, loads of a tile
+    static constexpr int RB = D * (BF16 ? 2 : 4);
+    const char *in;        // row of position x.start + i at in + i * in_t
+    char *pg;              // the block's page (rows of RB bytes)
+    long long in_t;
+    int page, pos_b, start, end, r, lr, lc;
+    Raw8<BF16> raw[NL];
+
+    __device__ BlockRows(const CacheArgs &a, const Tile &x, int h, int kv, int page_, int lane)
+    {
+        page = page_;
+        pos_b = x.pos / a.r * a.r;
+        start = x.start;
+        end = x.pos + x.n;
+        r = a.r;
+        in_t = (kv ? a.vt : a.kt) * (BF16 ? 2 : 4);
+        lr = lane / LPR;
+        lc = lane % LPR;
+        in = static_cast<const char *>(elem<BF16>(kv ? a.v : a.k, h * (kv ? a.vh : a.kh))) + x.row0 * in_t;
+        pg = static_cast<char *>(elem<BF16>(kv ? a.vp : a.kp, page_row(a, page, h, 0)));
+    }
+    __device__ int row_of(int row0, int i) const { return row0 + i * RPL + lr; }
+    // rows row0 .. of the block, zero where there is none; old: with those from before the call
+    __device__ void fetch(int row0, bool old)
+    {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int row = row_of(row0, i), pos = pos_b + row;
+            raw[i] = Raw8<BF16>();
+            if (row >= r) continue;   // (r = 16: half a tile)
+            if (pos >= start) {
+                if (pos < end) raw[i] = load_raw<BF16>(in + (long long)(pos - start) * in_t + RB / LPR * lc);
+            } else if (page >= 0 && old) {
+                raw[i] = load_raw<BF16>(pg + row * RB + RB / LPR * lc);
+            }
+        }
+    }
+    // the new ones (from `first` on) to the page
+    __device__ void keep(int row0, int first) const
+    {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int row = row_of(row0, i), pos = pos_b + row;
+            if (row < r && pos >= first && pos < end && page >= 0) store_raw<BF16>(pg + row * RB + RB / LPR * lc, raw[i]);
+        }
+    }
+    // to a wave's LDS tile of 32 rows (bf16: chunks swizzled for the transposing reads)
+    __device__ void stage(char *tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int tr = i * RPL + lr;
+            if constexpr (BF16) {
+                *reinterpret_cast<uint4 *>(tile + tr * RB + 16 * (lc ^ swzd<D>(tr))) =
+                    make_uint4(raw[i].w[0], raw[i].w[1], raw[i].w[2], raw[i].w[3]);
+            } else {
+                float f[8];
+                floats<BF16>(raw[i], f);
+                f32x4 *to = reinterpret_cast<f32x4 *>(tile + tr * RB + 32 * lc);
+                to[0] = f32x4{f[0], f[1], f[2], f[3]};
+                to[1] = f32x4{f[4], f[5], f[6], f[7]};
+            }
+        }
+    }
+};
+
+// weights of set e for the rows of block b
+__device__ inline const float *block_weights(const CacheArgs &a, int kv, int h, int e, int b)
+{
+    const int l = e / a.rank, s = e - l * a.rank;
+    const long long size = (long long)a.r << l;
+    return (kv ? a.wv : a.wk) + h * a.w_stride + a.rank * (size - a.r) + s * size + (long long)(b & ((1 << l) - 1)) * a.r;
+}
+
+// this lane's weights of a tile: rows 8 i + 4 (lane >> 5) + j of it in w[4 i + j]
+__device__ inline void tile_weights(const float *w, bool col, int row0, int r, int hh, float (&wf)[16])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f32x4u x = {0.f, 0.f, 0.f, 0.f};
+        if (col && row0 + 8 * i < r) x = *reinterpret_cast<const f32x4u *>(w + row0 + 8 * i + 4 * hh);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) wf[4 * i + j] = x[j];
+    }
+}
+
+template <bool BF16, int D>
+__device__ inline void tile_sums(const char *tile, const float (&wf)[16], int lane, f32x16 (&o)[D / 32])
+{
+    const int l32 = lane & 31, hh = lane >> 5;
+    if constexpr (BF16) {
+        const int gq = lane >> 4, s4 = lane & 15, jr = s4 >> 2, qq = s4 & 3;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            bf16x8 ws[3];   // each the rounding of what the ones before leave
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float left = wf[8 * hf + j];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    ws[k][j] = static_cast<__bf16>(left);
+                    left -= static_cast<float>(ws[k][j]);
+                }
+            }
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                s16x4 r[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int row = 16 * hf + 8 * k + 4 * (gq >> 1) + jr;
+                    const int off = row * D + ((8 * ((2 * (gq & 1) + (qq >> 1)) ^ swzd<D>(row)) + 4 * (qq & 1)) ^ (32 * db));
+                    r[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(reinterpret_cast<const __bf16 *>(tile) + off));
+                }
+                const s16x8 xv = {r[0][0], r[0][1], r[0][2], r[0][3], r[1][0], r[1][1], r[1][2], r[1][3]};
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xv), ws[k], o[db], 0, 0, 0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float *xr = reinterpret_cast<const float *>(tile) + grow(j, hh) * D + l32;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+                o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(xr[32 * db], wf[j], o[db], 0, 0, 0);
+        }
+    }
+}
+
+template <bool BF16, int D, int NW>
+union SumSmem {
+    __attribute__((aligned(16))) char tile[NW][32 * D * (BF16 ? 2 : 4)];
+    float part[NW][32][33];
 };
 
 // The summary of block b of key head h, complete with this call:
 //   S_e(b) = sum over its rows j of pi_e[b r mod s_l + j] x_j
 //            + (b starts a group of e's level ? 0 : S_e(b - 1)).
-// Rows from x.start on come from the caller's tensors, the others from the
-// block's page; d / 8 lanes hold a row, half of the waves the keys, the others
-// the values.  fp32 throughout: sums over up to 2^15 blocks of a group are kept.
-template <bool BF16, int D, int NT>
-__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, SumSmem<D, NT> &sm)
+// Half of the workgroup's NW waves take the keys, the others the values; each
+// half deals the block's 32-row tiles among its waves.  fp32 throughout: sums
+// over up to 2^15 blocks of a group are kept.  dst, before: the summary pages of
+// b and b - 1.
+template <bool BF16, int D, int NW>
+__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, int dst, int before,
+                                 SumSmem<BF16, D, NW> &sm)
 {
-    constexpr int LPR = D / 8, NW = NT / 64, HT = NT / 2, SLOTS = HT / LPR;
-    const int dst = summary_of(a, x.seq, b);
-    if (dst < 0) return;
-    const int before = b > 0 ? summary_of(a, x.seq, b - 1) : -1;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t = tid >= HT;
-    const int ch = 8 * (tid % LPR), slot = (tid - t * HT) / LPR;
-    const float *w = (t ? a.wv : a.wk) + h * a.w_stride;
-    const long long row = (long long)a.sets * D;   // floats of one tensor's sums
-    for (int e0 = 0; e0 < a.sets; e0 += kSumSets) {
-        float acc[kSumSets][8];
-        const float *we[kSumSets];
+    constexpr int HW = NW / 2;
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kv = wave / HW;
+    BlockRows<BF16, D> rows(a, x, h, kv, page, lane);
+    for (int s0 = 0; s0 < a.sets; s0 += 32) {
+        const bool col = s0 + l32 < a.sets;
+        const float *const w = block_weights(a, kv, h, col ? s0 + l32 : 0, b);
+        f32x16 o[D / 32];
 #pragma unroll
-        for (int e = 0; e < kSumSets; ++e) {
-            const int l = (e0 + e) / a.rank, s = (e0 + e) - l * a.rank;
-            const long long size = (long long)a.r << l;
-            we[e] = w + a.rank * (size - a.r) + s * size + (long long)(b & ((1 << l) - 1)) * a.r;
+        for (int db = 0; db < D / 32; ++db) o[db] = f32x16{0};
+        int row0 = 32 * (wave % HW);
+        float wf[16];
+        rows.fetch(row0, true);
+        tile_weights(w, col, row0, a.r, hh, wf);
+        while (row0 < a.r) {
+            rows.stage(sm.tile[wave]);
+            float now[16];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) acc[e][c] = 0.f;
+            for (int i = 0; i < 16; ++i) now[i] = wf[i];
+            row0 += 32 * HW;
+            rows.fetch(row0, true);
+            tile_weights(w, col, row0, a.r, hh, wf);
+            tile_sums<BF16, D>(sm.tile[wave], now, lane, o);
         }
-        for (int j = slot; j < a.r; j += SLOTS) {
-            const int pos = b * a.r + j;
-            float f[8];
-            if (pos >= x.start) {
-                const long long o = (long long)(x.row0 + pos - x.start) * (t ? a.vt : a.kt) + h * (t ? a.vh : a.kh);
-                load8f<BF16>(elem<BF16>(t ? a.v : a.k, o + ch), f);
-            } else if (page >= 0) {
-                load8f<BF16>(elem<BF16>(const_cast<const void *>(t ? a.vp : a.kp), page_row(a, page, h, j) + ch), f);
-            } else {
-                continue;
-            }
+        const int n = a.sets - s0 < 32 ? a.sets - s0 : 32;
 #pragma unroll
-            for (int e = 0; e < kSumSets; ++e) {
-                const float wj = e0 + e < a.sets ? we[e][j] : 0.f;
+        for (int db = 0; db < D / 32; ++db) {
+            __syncthreads();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) acc[e][c] = fmaf(wj, f[c], acc[e][c]);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < kSumSets; ++e)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-#pragma unroll
-                for (int m = LPR; m < 64; m *= 2) acc[e][c] += __shfl_xor(acc[e][c], m);
-                if (lane < LPR) sm.part[wave][e][ch + c] = acc[e][c];
-            }
-        __syncthreads();
-        for (int i = tid; i < 2 * kSumSets * D; i += NT) {
-            const int kv = i / (kSumSets * D), e = i / D % kSumSets, c = i % D;
-            if (e0 + e < a.sets) {
+            for (int j = 0; j < 16; ++j) sm.part[wave][l32][grow(j, hh)] = o[db][j];
+            __syncthreads();
+            for (int i = tid; i < 2 * 32 * n; i += 64 * NW) {
+                const int c = i & 31, t = (i >> 5) & 1, e = i >> 6;
                 float s = 0.f;
 #pragma unroll
-                for (int k = 0; k < NW / 2; ++k) s += sm.part[kv * (NW / 2) + k][e][c];
-                const long long o = kv * row + (long long)(e0 + e) * D + c;
-                if (before >= 0 && (b & ((1 << ((e0 + e) / a.rank)) - 1)))
-                    s += a.sum[((long long)before * a.kv_heads + h) * 2 * row + o];
-                a.sum[((long long)dst * a.kv_heads + h) * 2 * row + o] = s;
+                for (int k = 0; k < HW; ++k) s += sm.part[t * HW + k][e][c];
+                const long long off = ((long long)t * a.sets + s0 + e) * D + 32 * db + c, head = 2LL * a.sets * D;
+                if (before >= 0 && (b & ((1 << ((s0 + e) / a.rank)) - 1)))
+                    s += a.sum[((long long)before * a.kv_heads + h) * head + off];
+                a.sum[((long long)dst * a.kv_heads + h) * head + off] = s;
             }
         }
         __syncthreads();

@@ -227,3 +227,28 @@ def test_launches_cover_every_tile(tiling):
         tpb = -(-r // tm)
         tiles = [tiling.host_cache_tile_of(r, tm, tpb, p) for p in range(3 * r)]
         assert tiles == [p // r * tpb + p % r // tm for p in range(3 * r)]
+
+
+def test_tiles_of_query_heads(tiling):
+    """Every query head has one workgroup, which holds at most 32 of them; a
+    tile holds at most 128 rows and a block few tiles more than it must."""
+    out = (ctypes.c_int * 4)()
+    for r in (16, 32, 64, 128, 192, 256):
+        for group in range(1, 200):
+            tiling.host_cache_route(r, group, 1, r, 10 * r, 256, out)
+            _, gs, split, tm = out[:]
+            assert 1 <= gs <= 32 and (split - 1) * gs < group <= split * gs
+            assert 1 <= tm <= r and tm * gs <= 128
+            assert -(-r // tm) <= 2 * -(-r * gs // 128)
+
+
+@pytest.mark.parametrize("args,route", [
+    ((128, 1, 16, 1, 1), 0), ((128, 4, 4, 1, 100), 0), ((128, 1, 8, 4, 40), 0),    # up to four rows per key head
+    ((128, 5, 4, 1, 100), 1), ((128, 1, 16, 5, 2000), 1), ((128, 8, 16, 4, 9000), 1),   # one tile of 32
+    ((128, 1, 16, 128, 1024), 1), ((128, 1, 16, 4096, 2000), 1),                   # too few rows for the device
+    ((128, 1, 16, 128, 2048), 2), ((64, 4, 4, 2500, 8000), 2), ((16, 1, 16, 400, 400), 2)])
+def test_routes(tiling, args, route):
+    out = (ctypes.c_int * 4)()
+    r, group, kv, chunk, rows = args
+    tiling.host_cache_route(r, group, kv, chunk, rows, 256, out)
+    assert out[0] == route

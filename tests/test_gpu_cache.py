@@ -144,6 +144,44 @@ def test_pieces_and_tokens(shape, dtype, how):
     s.check_pages()
 
 
+ROWS = [  # as above, with key heads enough that the device's waves take rows
+    (32, 32, 64, 64, 1), (32, 16, 32, 16, 2), (48, 16, 128, 128, 1), (40, 8, 64, 192, 1), (64, 64, 128, 32, 4),
+    (66, 2, 32, 64, 1), (32, 16, 64, 256, 2),
+]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("shape", ROWS, ids=lambda s: "-".join(map(str, s)))
+def test_longer_pieces(shape, dtype):
+    """Pieces of enough rows that the waves of a workgroup take different ones."""
+    H, kv, d, r, rank = shape
+    n = max(9 * r + 5, 1200)
+    s = Served([n, n // 2, 40, 1], H, kv, d, r, rank, dtype=DT[dtype])
+    s.step([n - r - 3, n // 2 - 50, 40, 0], pad=3)
+    s.step([r, 33, 0, 1], "two")
+    s.step([3, 17, 0, 0])
+    s.check_pages()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_longer_pieces_with_missing_pages(dtype):
+    """A missing page hides its tokens there too; rows of no sequence stay."""
+    r, n, kv = 32, 900, 16
+    s = Served([n], kv, kv, 64, r, 1, dtype=DT[dtype])
+    s.step([n], "append")
+    q, b = s.rows(s.q, [n], start=[0], pad=2), s.batch([n], start=[0])
+    gone = (3, 4, 11)
+    for x in gone:
+        b.page_table[0, x] = -1 if x != 4 else s.pages.k.shape[0]
+    out = torch.full_like(q, 7.0)
+    s.op.attend(q, s.pages, b, out=out)
+    assert (out[n:] == 7.0).all()
+    for h in (0, kv - 1):
+        ref, bound = R.attend(s.q[0][:, h], s.k[0][:, h], s.v[0][:, h], s.wk[h], s.wv[h], r, 1, s.levels, 64 ** -0.5,
+                              DT[dtype], missing=gone)
+        assert ((out[:n, h].double().cpu() - ref).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 def test_token_by_token(dtype):
     s = Served([16 * 11 + 3, 16 * 4], 2, 1, 32, 16, 1, max_len=16 * 16, dtype=DT[dtype], seed=2)
