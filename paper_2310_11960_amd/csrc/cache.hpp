@@ -93,6 +93,42 @@ inline CacheRoute cache_route(const CacheArgs &a, int cus)
     return most * c.gs <= 32 || groups < cus ? CACHE_KEYS : CACHE_ROWS;
 }
 
+// Workgroups are numbered tile by tile, a tile's key heads one after the other: a
+// sequence that has more to do than others (a finished block's sums) is not
+// last with every head, and with a multiple of eight heads the neighbouring
+// tiles of one head, which share rows, meet in one XCD's L2.
+struct CacheGroup {
+    unsigned unit;
+    int head;
+};
+__device__ inline CacheGroup cache_group(int heads)
+{
+    CacheGroup g;
+    g.unit = blockIdx.x / (unsigned)heads;
+    g.head = (int)(blockIdx.x - g.unit * (unsigned)heads);
+    return g;
+}
+
+// Tile positions of the launches and the key-head parts of a tile.
+inline int token_tile(const CacheArgs &a) { return a.max_chunk < a.rows ? a.max_chunk : a.rows; }
+inline int keys_tile(const ChunkShape &c) { return 32 / c.gs; }
+
+// Threads of a launch stay below 2^32.
+inline bool cache_launches_fit(const CacheArgs &a, bool appends, bool attends, int cus)
+{
+    auto fits = [&](int tm, long long heads, int threads) {
+        return make_tiling(a, tm).units <= 0xffffffffLL / threads / heads;
+    };
+    if (appends && !fits(a.r, a.kv_heads, 256)) return false;
+    if (!attends) return true;
+    const ChunkShape c = chunk_shape(a);
+    switch (cache_route(a, cus)) {
+    case CACHE_TOKENS: return fits(token_tile(a), a.kv_heads, 512);
+    case CACHE_KEYS: return fits(keys_tile(c), (long long)a.kv_heads * c.split, 512);
+    default: return fits(c.tm, (long long)a.kv_heads * c.split, 256);
+    }
+}
+
 hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
 hipError_t launch_cache_token(const CacheArgs &a, hipStream_t st);
 hipError_t launch_cache_keys(const CacheArgs &a, const ChunkShape &c, hipStream_t st);

@@ -20,7 +20,7 @@ struct fma_cache_plan_s {
 
 namespace {
 
-// Tokens and sequences of one call: workgroups x threads of a launch stay below 2^32.
+// Tokens and sequences of one call.
 constexpr int64_t kMaxRows = 1 << 21;
 constexpr int32_t kMaxSequences = 1 << 20;
 
@@ -116,6 +116,8 @@ fma_status_t check_call(const Call &c, CacheArgs &a, bool *skip)
     a.r = d.block, a.rank = d.rank, a.levels = c.p->levels, a.sets = sets;
     a.head_dim = d.head_dim, a.bf16 = d.dtype == FMA_BF16;
     a.scale_log2 = c.p->scale * (float)M_LOG2E;
+    if (!cache_launches_fit(a, writes, attends, compute_units()))
+        return set_status(FMA_ERR_SHAPE, "%s: too many rows and heads for one call", fn);
     (void)hipGetLastError();
     return FMA_OK;
 }

@@ -22,15 +22,16 @@ constexpr int kThreads = 256;
 template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads) void cache_append_kernel(CacheArgs a, Tiling t)
 {
-    __shared__ SumSmem<BF16, D, kThreads / 64> sm;
+    __shared__ __attribute__((aligned(16))) char lds[kThreads / 64][kSumTile<BF16>];
     Tile x;
-    if (!find_tile(a, t, blockIdx.x, x)) return;
-    const int h = blockIdx.y, b = x.pos / a.r;
+    const CacheGroup g = cache_group(a.kv_heads);
+    if (!find_tile(a, t, g.unit, x)) return;
+    const int h = g.head, b = x.pos / a.r;
     const int page = page_of(a, x.seq, b);
     copy_rows<BF16, D, kThreads>(a, x, h, page);
     if (!a.sets || (x.pos + x.n) % a.r) return;
     const int dst = summary_of(a, x.seq, b), before = b > 0 ? summary_of(a, x.seq, b - 1) : -1;
-    if (dst >= 0) summarize<BF16, D, kThreads / 64>(a, x, h, b, page, dst, before, sm);
+    if (dst >= 0) summarize<BF16, D, kThreads / 64>(a, x, h, b, page, dst, before, lds[threadIdx.x >> 6]);
 }
 
 // Pass 1.  Workgroup: a block and two key heads (waves 0, 1: keys, values of the
@@ -40,18 +41,19 @@ template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads) void cache_blocks_kernel(CacheArgs a, Tiling t)
 {
     constexpr int ND = D / 32;
-    __shared__ __attribute__((aligned(16))) char lds[kThreads / 64][32 * BlockRows<BF16, D>::RB];
+    __shared__ __attribute__((aligned(16))) char lds[kThreads / 64][32 * D * (BF16 ? 2 : 4)];
     Tile x;
-    if (!find_tile(a, t, blockIdx.x, x)) return;
+    const CacheGroup g = cache_group((a.kv_heads + 1) / 2);
+    if (!find_tile(a, t, g.unit, x)) return;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = 2 * blockIdx.y + (wave >> 1), kv = wave & 1;
+    const int h = 2 * g.head + (wave >> 1), kv = wave & 1;
     if (h >= a.kv_heads) return;
     const int b = x.pos / a.r;
     const bool done = a.sets && x.pos + x.n == (b + 1) * a.r;
     const int dst = done ? summary_of(a, x.seq, b) : -1;
     char *const tile = lds[wave];
-    BlockRows<BF16, D> rows(a, x, h, kv, page_of(a, x.seq, b), lane);
+    BlockRows<BF16, D, D> rows(a, x, h, kv, page_of(a, x.seq, b), 0, lane);
 
     for (int s0 = 0; s0 == 0 || s0 < a.sets; s0 += 32) {
         const bool col = dst >= 0 && s0 + l32 < a.sets;
@@ -126,11 +128,11 @@ hipError_t append_d(const CacheArgs &a, hipStream_t st)
 {
     const Tiling t = make_tiling(a, a.r);
     if (a.max_chunk <= a.r) {
-        hipLaunchKernelGGL((cache_append_kernel<BF16, D>), dim3((unsigned)t.units, a.kv_heads), dim3(kThreads), 0, st, a, t);
+        hipLaunchKernelGGL((cache_append_kernel<BF16, D>), dim3((unsigned)(t.units * a.kv_heads)), dim3(kThreads), 0, st, a, t);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((cache_blocks_kernel<BF16, D>), dim3((unsigned)t.units, (a.kv_heads + 1) / 2), dim3(kThreads), 0, st,
-                       a, t);
+    hipLaunchKernelGGL((cache_blocks_kernel<BF16, D>), dim3((unsigned)(t.units * ((a.kv_heads + 1) / 2))), dim3(kThreads),
+                       0, st, a, t);
     if (a.levels > 1)
         hipLaunchKernelGGL(cache_scan_kernel, dim3(a.S, a.kv_heads, (2 * a.sets * D / 4 + 63) / 64), dim3(64), 0, st, a);
     return hipGetLastError();

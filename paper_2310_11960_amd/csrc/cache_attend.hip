@@ -26,7 +26,7 @@ struct AttendSmem {
     union {
         __attribute__((aligned(16))) char v[NW][32 * D * (BF16 ? 2 : 4)];
         float o[NW][32][33];
-        SumSmem<BF16, D, NW> sum;
+        __attribute__((aligned(16))) char sum[NW][kSumTile<BF16>];
     };
     float m[NW][32], l[NW][32];
 };
@@ -37,10 +37,11 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
     constexpr int NT = 64 * NW, ND = D / 32, NC = BF16 ? D / 16 : D / 8;   // 16-byte pieces of a lane's half row
     __shared__ AttendSmem<BF16, D, NW> sm;
     Tile x;
-    if (!find_tile(a, t, blockIdx.x, x)) return;
+    const CacheGroup g = cache_group(a.kv_heads * split);
+    if (!find_tile(a, t, g.unit, x)) return;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = blockIdx.y / split, g0 = (blockIdx.y - h * split) * gs;
+    const int h = g.head / split, g0 = (g.head - h * split) * gs;
     const int ng = gs < a.group - g0 ? gs : a.group - g0;   // this workgroup's query heads
     const int b = x.pos / a.r, pos_b = b * a.r;
     const int page = page_of(a, x.seq, b), page0 = b > 0 ? page_of(a, x.seq, b - 1) : -1;
@@ -94,9 +95,9 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
             }
         } else {
             const int slot = 32 * (i - near) + l32, e = slot < nfar ? slot >> 1 : 0, lv = e / a.rank;
-            const int q = b >> lv, g = q - 2 - (slot & 1);
-            valid = slot < nfar && g >= 0 && (!(slot & 1) || (q & 1));
-            const int sp = valid ? summary_of(a, x.seq, ((g + 1) << lv) - 1) : -1;
+            const int q = b >> lv, fg = q - 2 - (slot & 1);
+            valid = slot < nfar && fg >= 0 && (!(slot & 1) || (q & 1));
+            const int sp = valid ? summary_of(a, x.seq, ((fg + 1) << lv) - 1) : -1;
             valid = sp >= 0;
             const float *kr = a.sum + (((long long)sp * a.kv_heads + h) * 2 * a.sets + e) * D;
             const float *vr = kr + (long long)a.sets * D;
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
     if (a.write && g0 == 0 && a.sets && kend % a.r == 0) {
         const int dst = summary_of(a, x.seq, b), before = b > 0 ? summary_of(a, x.seq, b - 1) : -1;
         __syncthreads();
-        if (dst >= 0) summarize<BF16, D, NW>(a, x, h, b, page, dst, before, sm.sum);
+        if (dst >= 0) summarize<BF16, D, NW>(a, x, h, b, page, dst, before, sm.sum[wave]);
     }
 }
 
@@ -246,8 +247,8 @@ template <bool BF16, int D>
 hipError_t attend_d(const CacheArgs &a, const ChunkShape &c, hipStream_t st)
 {
     constexpr int NW = BF16 ? 8 : 4;
-    const Tiling t = make_tiling(a, 32 / c.gs);
-    hipLaunchKernelGGL((cache_attend_kernel<BF16, D, NW>), dim3((unsigned)t.units, a.kv_heads * c.split), dim3(64 * NW), 0,
+    const Tiling t = make_tiling(a, keys_tile(c));
+    hipLaunchKernelGGL((cache_attend_kernel<BF16, D, NW>), dim3((unsigned)(t.units * a.kv_heads * c.split)), dim3(64 * NW), 0,
                        st, a, t, c.split, c.gs);
     return hipGetLastError();
 }

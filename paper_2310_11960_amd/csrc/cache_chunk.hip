@@ -33,10 +33,11 @@ __global__ __launch_bounds__(64 * NW) void cache_chunk_kernel(CacheArgs a, Tilin
     constexpr int P = ChunkSmem<BF16, D>::P;
     __shared__ ChunkSmem<BF16, D> sm;
     Tile x;
-    if (!find_tile(a, t, blockIdx.x, x)) return;
+    const CacheGroup g = cache_group(a.kv_heads * split);
+    if (!find_tile(a, t, g.unit, x)) return;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = blockIdx.y / split, g0 = (blockIdx.y - h * split) * gs;
+    const int h = g.head / split, g0 = (g.head - h * split) * gs;
     const int ng = gs < a.group - g0 ? gs : a.group - g0;
     const int b = x.pos / a.r, pos_b = b * a.r;
     const int page = page_of(a, x.seq, b), page0 = b > 0 ? page_of(a, x.seq, b - 1) : -1;

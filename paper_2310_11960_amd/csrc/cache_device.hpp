@@ -81,22 +81,22 @@ __device__ inline void copy_rows(const CacheArgs &a, const Tile &x, int h, int p
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // the caller's weights
 
-// One wave's share of a block's sums: the block's rows (keys or values of head
-// h), 32 at a time, against the weights of sets s0 .. s0 + 31,
+// One wave's share of a block's sums: C channels of the block's rows (keys or
+// values of head h), 32 rows at a time, against the weights of 32 sets,
 //   o[db] += X^T W^T      (rows: channels 32 db .., columns: sets),
 // on the matrix cores.  fp32 weights meet bf16 rows exactly: each weight is
 // split into three bf16 terms (8 + 8 + 8 bits), so the sums keep fp32 accuracy.
-template <bool BF16, int D>
+template <bool BF16, int D, int C>
 struct BlockRows {
-    static constexpr int LPR = D / 8, RPL = 64 / LPR, NL = 32 / RPL, ND = D / 32;   // rows of a load, loads of a tile
-    static constexpr int RB = D * (BF16 ? 2 : 4);
+    static constexpr int LPR = C / 8, RPL = 64 / LPR, NL = 32 / RPL;   // rows of a load, loads of a tile
+    static constexpr int RB = D * (BF16 ? 2 : 4), TB = C * (BF16 ? 2 : 4), LB = TB / LPR;   // bytes of a row, in a tile, a lane
     const char *in;        // row of position x.start + i at in + i * in_t
     char *pg;              // the block's page (rows of RB bytes)
     long long in_t;
     int page, pos_b, start, end, r, lr, lc;
     Raw8<BF16> raw[NL];
 
-    __device__ BlockRows(const CacheArgs &a, const Tile &x, int h, int kv, int page_, int lane)
+    __device__ BlockRows(const CacheArgs &a, const Tile &x, int h, int kv, int page_, int c0, int lane)   // c0: first channel
     {
         page = page_;
         pos_b = x.pos / a.r * a.r;
@@ -106,8 +106,8 @@ struct BlockRows {
         in_t = (kv ? a.vt : a.kt) * (BF16 ? 2 : 4);
         lr = lane / LPR;
         lc = lane % LPR;
-        in = static_cast<const char *>(elem<BF16>(kv ? a.v : a.k, h * (kv ? a.vh : a.kh))) + x.row0 * in_t;
-        pg = static_cast<char *>(elem<BF16>(kv ? a.vp : a.kp, page_row(a, page, h, 0)));
+        in = static_cast<const char *>(elem<BF16>(kv ? a.v : a.k, h * (kv ? a.vh : a.kh) + c0)) + x.row0 * in_t;
+        pg = static_cast<char *>(elem<BF16>(kv ? a.vp : a.kp, page_row(a, page, h, 0) + c0));
     }
     __device__ int row_of(int row0, int i) const { return row0 + i * RPL + lr; }
     // rows row0 .. of the block, zero where there is none; old: with those from before the call
@@ -119,9 +119,9 @@ struct BlockRows {
             raw[i] = Raw8<BF16>();
             if (row >= r) continue;   // (r = 16: half a tile)
             if (pos >= start) {
-                if (pos < end) raw[i] = load_raw<BF16>(in + (long long)(pos - start) * in_t + RB / LPR * lc);
+                if (pos < end) raw[i] = load_raw<BF16>(in + (long long)(pos - start) * in_t + LB * lc);
             } else if (page >= 0 && old) {
-                raw[i] = load_raw<BF16>(pg + row * RB + RB / LPR * lc);
+                raw[i] = load_raw<BF16>(pg + row * RB + LB * lc);
             }
         }
     }
@@ -131,7 +131,7 @@ struct BlockRows {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int row = row_of(row0, i), pos = pos_b + row;
-            if (row < r && pos >= first && pos < end && page >= 0) store_raw<BF16>(pg + row * RB + RB / LPR * lc, raw[i]);
+            if (row < r && pos >= first && pos < end && page >= 0) store_raw<BF16>(pg + row * RB + LB * lc, raw[i]);
         }
     }
     // to a wave's LDS tile of 32 rows (bf16: chunks swizzled for the transposing reads)
@@ -141,12 +141,12 @@ struct BlockRows {
         for (int i = 0; i < NL; ++i) {
             const int tr = i * RPL + lr;
             if constexpr (BF16) {
-                *reinterpret_cast<uint4 *>(tile + tr * RB + 16 * (lc ^ swzd<D>(tr))) =
+                *reinterpret_cast<uint4 *>(tile + tr * TB + 16 * (lc ^ swzd<C>(tr))) =
                     make_uint4(raw[i].w[0], raw[i].w[1], raw[i].w[2], raw[i].w[3]);
             } else {
                 float f[8];
                 floats<BF16>(raw[i], f);
-                f32x4 *to = reinterpret_cast<f32x4 *>(tile + tr * RB + 32 * lc);
+                f32x4 *to = reinterpret_cast<f32x4 *>(tile + tr * TB + 32 * lc);
                 to[0] = f32x4{f[0], f[1], f[2], f[3]};
                 to[1] = f32x4{f[4], f[5], f[6], f[7]};
             }
@@ -174,8 +174,8 @@ __device__ inline void tile_weights(const float *w, bool col, int row0, int r, i
     }
 }
 
-template <bool BF16, int D>
-__device__ inline void tile_sums(const char *tile, const float (&wf)[16], int lane, f32x16 (&o)[D / 32])
+template <bool BF16, int C>
+__device__ inline void tile_sums(const char *tile, const float (&wf)[16], int lane, f32x16 (&o)[C / 32])
 {
     const int l32 = lane & 31, hh = lane >> 5;
     if constexpr (BF16) {
@@ -193,12 +193,12 @@ __device__ inline void tile_sums(const char *tile, const float (&wf)[16], int la
                 }
             }
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
+            for (int db = 0; db < C / 32; ++db) {
                 s16x4 r[2];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int row = 16 * hf + 8 * k + 4 * (gq >> 1) + jr;
-                    const int off = row * D + ((8 * ((2 * (gq & 1) + (qq >> 1)) ^ swzd<D>(row)) + 4 * (qq & 1)) ^ (32 * db));
+                    const int off = row * C + ((8 * ((2 * (gq & 1) + (qq >> 1)) ^ swzd<C>(row)) + 4 * (qq & 1)) ^ (32 * db));
                     r[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(reinterpret_cast<const __bf16 *>(tile) + off));
                 }
                 const s16x8 xv = {r[0][0], r[0][1], r[0][2], r[0][3], r[1][0], r[1][1], r[1][2], r[1][3]};
@@ -210,74 +210,67 @@ __device__ inline void tile_sums(const char *tile, const float (&wf)[16], int la
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float *xr = reinterpret_cast<const float *>(tile) + grow(j, hh) * D + l32;
+            const float *xr = reinterpret_cast<const float *>(tile) + grow(j, hh) * C + l32;
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db)
+            for (int db = 0; db < C / 32; ++db)
                 o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(xr[32 * db], wf[j], o[db], 0, 0, 0);
         }
     }
 }
 
-template <bool BF16, int D, int NW>
-union SumSmem {
-    __attribute__((aligned(16))) char tile[NW][32 * D * (BF16 ? 2 : 4)];
-    float part[NW][32][33];
-};
+// LDS of a wave that sums blocks 32 channels at a time
+template <bool BF16>
+constexpr int kSumTile = 32 * 32 * (BF16 ? 2 : 4);
 
 // The summary of block b of key head h, complete with this call:
-//   S_e(b) = sum over its rows j of pi_e[b r mod s_l + j] x_j
-//            + (b starts a group of e's level ? 0 : S_e(b - 1)).
-// Half of the workgroup's NW waves take the keys, the others the values; each
-// half deals the block's 32-row tiles among its waves.  fp32 throughout: sums
-// over up to 2^15 blocks of a group are kept.  dst, before: the summary pages of
-// b and b - 1.
+//   S_e(b) = (b starts a group of e's level ? 0 : S_e(b - 1))
+//            + sum over its rows j of pi_e[b r mod s_l + j] x_j.
+// A wave takes 32 channels of the keys or of the values, its sums start from the
+// previous block's, and no two waves meet.  fp32 throughout: sums over up to 2^15
+// blocks of a group are kept.  dst, before: the summary pages of b and b - 1.
 template <bool BF16, int D, int NW>
-__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, int dst, int before,
-                                 SumSmem<BF16, D, NW> &sm)
+__device__ inline void summarize(const CacheArgs &a, const Tile &x, int h, int b, int page, int dst, int before, char *tile)
 {
-    constexpr int HW = NW / 2;
-    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kv = wave / HW;
-    BlockRows<BF16, D> rows(a, x, h, kv, page, lane);
-    for (int s0 = 0; s0 < a.sets; s0 += 32) {
-        const bool col = s0 + l32 < a.sets;
-        const float *const w = block_weights(a, kv, h, col ? s0 + l32 : 0, b);
-        f32x16 o[D / 32];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll 1
+    for (int task = wave; task < 2 * (D / 32); task += NW) {
+        const int kv = task & 1, c0 = 32 * (task >> 1);
+        BlockRows<BF16, D, 32> rows(a, x, h, kv, page, c0, lane);
+#pragma unroll 1
+        for (int s0 = 0; s0 < a.sets; s0 += 32) {
+            const int e = s0 + l32;
+            const bool col = e < a.sets;
+            const float *const w = block_weights(a, kv, h, col ? e : 0, b);
+            float next[16];
+            rows.fetch(0, true);
+            tile_weights(w, col, 0, a.r, hh, next);
+            f32x16 o[1] = {f32x16{0}};
+            if (col && before >= 0 && (b & ((1 << (e / a.rank)) - 1))) {
+                const float *const from = a.sum + ((((long long)before * a.kv_heads + h) * 2 + kv) * a.sets + e) * D + c0;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[db] = f32x16{0};
-        int row0 = 32 * (wave % HW);
-        float wf[16];
-        rows.fetch(row0, true);
-        tile_weights(w, col, row0, a.r, hh, wf);
-        while (row0 < a.r) {
-            rows.stage(sm.tile[wave]);
-            float now[16];
+                for (int j = 0; j < 16; j += 4) {
+                    const f32x4 f = *reinterpret_cast<const f32x4 *>(from + grow(j, hh));
+                    o[0][j] = f[0], o[0][j + 1] = f[1], o[0][j + 2] = f[2], o[0][j + 3] = f[3];
+                }
+            }
+#pragma unroll 1
+            for (int row0 = 0; row0 < a.r; row0 += 32) {
+                float wf[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) now[i] = wf[i];
-            row0 += 32 * HW;
-            rows.fetch(row0, true);
-            tile_weights(w, col, row0, a.r, hh, wf);
-            tile_sums<BF16, D>(sm.tile[wave], now, lane, o);
-        }
-        const int n = a.sets - s0 < 32 ? a.sets - s0 : 32;
+                for (int j = 0; j < 16; ++j) wf[j] = next[j];
+                rows.stage(tile);
+                rows.fetch(row0 + 32, true);
+                tile_weights(w, col, row0 + 32, a.r, hh, next);
+                tile_sums<BF16, 32>(tile, wf, lane, o);
+            }
+            if (col) {
+                float *const to = a.sum + ((((long long)dst * a.kv_heads + h) * 2 + kv) * a.sets + e) * D + c0;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) sm.part[wave][l32][grow(j, hh)] = o[db][j];
-            __syncthreads();
-            for (int i = tid; i < 2 * 32 * n; i += 64 * NW) {
-                const int c = i & 31, t = (i >> 5) & 1, e = i >> 6;
-                float s = 0.f;
-#pragma unroll
-                for (int k = 0; k < HW; ++k) s += sm.part[t * HW + k][e][c];
-                const long long off = ((long long)t * a.sets + s0 + e) * D + 32 * db + c, head = 2LL * a.sets * D;
-                if (before >= 0 && (b & ((1 << ((s0 + e) / a.rank)) - 1)))
-                    s += a.sum[((long long)before * a.kv_heads + h) * head + off];
-                a.sum[((long long)dst * a.kv_heads + h) * head + off] = s;
+                for (int j = 0; j < 16; j += 4)
+                    *reinterpret_cast<f32x4 *>(to + grow(j, hh)) = f32x4{o[0][j], o[0][j + 1], o[0][j + 2], o[0][j + 3]};
             }
         }
-        __syncthreads();
     }
 }
 

@@ -22,7 +22,7 @@ template <bool BF16, int D, int R>
 struct TokenSmem {
     union {
         float o[kWaves][R][D];
-        SumSmem<BF16, D, kWaves> sum;
+        __attribute__((aligned(16))) char sum[kWaves][kSumTile<BF16>];
     };
     float m[kWaves][R], l[kWaves][R];
 };
@@ -59,10 +59,11 @@ __global__ __launch_bounds__(kThreads) void cache_token_kernel(CacheArgs a, Tili
     constexpr int LPR = D / 8, RPG = 64 / LPR, U = 4;   // rows of a wave's load
     __shared__ TokenSmem<BF16, D, R> sm;
     Tile x;
-    if (!find_tile(a, t, blockIdx.x, x)) return;
+    const CacheGroup cg = cache_group(a.kv_heads);
+    if (!find_tile(a, t, cg.unit, x)) return;
     const int tid = threadIdx.x, lane = tid & 63, slot = lane / LPR, ch = 8 * (lane % LPR);
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = blockIdx.y, b = x.pos / a.r, pos_b = b * a.r;
+    const int h = cg.head, b = x.pos / a.r, pos_b = b * a.r;
     const int page = page_of(a, x.seq, b), page0 = b > 0 ? page_of(a, x.seq, b - 1) : -1;
     const int nrow = x.n * a.group;
 
@@ -243,17 +244,16 @@ __global__ __launch_bounds__(kThreads) void cache_token_kernel(CacheArgs a, Tili
     }
     if (dst >= 0) {
         __syncthreads();
-        summarize<BF16, D, kWaves>(a, x, h, b, page, dst, before, sm.sum);
+        summarize<BF16, D, kWaves>(a, x, h, b, page, dst, before, sm.sum[wave]);
     }
 }
 
 template <bool BF16, int D>
 hipError_t token_d(const CacheArgs &a, hipStream_t st)
 {
-    const int most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
-    const Tiling t = make_tiling(a, most);
-    const dim3 grid((unsigned)t.units, a.kv_heads);
-    switch (most * a.group) {
+    const Tiling t = make_tiling(a, token_tile(a));
+    const dim3 grid((unsigned)(t.units * a.kv_heads));
+    switch (token_tile(a) * a.group) {
     case 1: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 1>), grid, dim3(kThreads), 0, st, a, t); break;
     case 2: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 2>), grid, dim3(kThreads), 0, st, a, t); break;
     default: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 4>), grid, dim3(kThreads), 0, st, a, t); break;
