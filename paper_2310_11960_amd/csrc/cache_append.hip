@@ -84,41 +84,46 @@ __global__ __launch_bounds__(kThreads) void cache_blocks_kernel(CacheArgs a, Til
     }
 }
 
-// Pass 2: thread (sequence, head, four channels of a set) walks the blocks that
-// the call completed, kScan of them on their way at a time.
-constexpr int kScan = 16;
+// Pass 2: thread (sequence, head, channel of a set) walks the blocks that the call
+// completed, kScan of them on their way at a time; a wave's block is uniform.
+// Two prompts of 98K tokens together, 16 heads, leave 512 waves: it takes 16 KB in
+// flight in each to keep HBM busy (kScan 16 with four channels a thread, 128
+// waves: 93 us).
+constexpr int kScan = 64;   // lanes of a wave
 
-__global__ __launch_bounds__(64) void cache_scan_kernel(CacheArgs a)
+__global__ __launch_bounds__(kThreads) void cache_scan_kernel(CacheArgs a)
 {
-    const int seq = blockIdx.x, h = blockIdx.y;
-    const int col = 4 * (blockIdx.z * 64 + threadIdx.x), cols = 2 * a.sets * a.head_dim;
-    if (col >= cols) return;
-    const int c0 = a.cu[seq], c1 = a.cu[seq + 1], s = a.start[seq];
+    const int seq = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
+    const int cols = 2 * a.sets * a.head_dim, at = blockIdx.z * kThreads + threadIdx.x;
+    const int col = at < cols ? at : 0;   // (whole waves stay: every lane holds a block's page)
+    const int c0 = listed(a.cu, seq), c1 = listed(a.cu, seq + 1), s = listed(a.start, seq);
     if (!sequence_fits(a, c0, c1, s)) return;
     const int l = col / a.head_dim % a.sets / a.rank;
-    if (l == 0) return;   // a group of level 1 is one block
+    const bool live = at < cols && l > 0;   // a group of level 1 is one block
     const int b0 = s / a.r, b1 = (s + c1 - c0) / a.r;
     if (b0 == b1) return;
-    auto at = [&](int b) -> f32x4 * {
-        const int p = b >= 0 && b < b1 ? summary_of(a, seq, b) : -1;
-        return p < 0 ? nullptr : reinterpret_cast<f32x4 *>(a.sum + ((long long)p * a.kv_heads + h) * cols + col);
-    };
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    const f32x4 *const prev = at(b0 - 1);
-    f32x4 acc = prev ? *prev : zero;
+    float *const base = a.sum + (long long)h * cols;
+    const long long page = (long long)a.kv_heads * cols;
+    const int prev = b0 > 0 ? summary_of(a, seq, b0 - 1) : -1;
+    float acc = prev >= 0 ? (base + prev * page)[col] : 0.f;
     for (int b = b0; b < b1; b += kScan) {
-        f32x4 *p[kScan], own[kScan];
-#pragma unroll
-        for (int i = 0; i < kScan; ++i) p[i] = at(b + i);
-#pragma unroll
-        for (int i = 0; i < kScan; ++i) own[i] = p[i] ? *p[i] : zero;
+        const int mine = b + lane < b1 ? summary_of(a, seq, b + lane) : -1;   // lane i: page of block b + i
+        float own[kScan];
 #pragma unroll
         for (int i = 0; i < kScan; ++i) {
+            own[i] = 0.f;
+            const int p = __builtin_amdgcn_readlane(mine, i);
+            if (p >= 0 && live) own[i] = (base + p * page)[col];
+        }
+#pragma unroll
+        for (int i = 0; i < kScan; ++i) {
+            if (b + i >= b1) break;
+            const int p = __builtin_amdgcn_readlane(mine, i);
             acc = (b + i) & ((1 << l) - 1) ? acc + own[i] : own[i];
-            if (p[i])
-                *p[i] = acc;
-            else
-                acc = zero;   // the sums of a missing page count as zero
+            if (p < 0)
+                acc = 0.f;   // the sums of a missing page count as zero
+            else if (live)
+                (base + p * page)[col] = acc;
         }
     }
 }
@@ -134,7 +139,8 @@ hipError_t append_d(const CacheArgs &a, hipStream_t st)
     hipLaunchKernelGGL((cache_blocks_kernel<BF16, D>), dim3((unsigned)(t.units * ((a.kv_heads + 1) / 2))), dim3(kThreads),
                        0, st, a, t);
     if (a.levels > 1)
-        hipLaunchKernelGGL(cache_scan_kernel, dim3(a.S, a.kv_heads, (2 * a.sets * D / 4 + 63) / 64), dim3(64), 0, st, a);
+        hipLaunchKernelGGL(cache_scan_kernel, dim3(a.S, a.kv_heads, (2 * a.sets * D + kThreads - 1) / kThreads), dim3(kThreads),
+                           0, st, a);
     return hipGetLastError();
 }
 

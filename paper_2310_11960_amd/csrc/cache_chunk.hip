@@ -26,7 +26,7 @@ struct ChunkSmem {
 };
 
 template <bool BF16, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs)
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 ? 1 : D == 128 ? 2 : 3))) void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs)
 {
     constexpr int NT = 64 * NW, ND = D / 32, NC = BF16 ? D / 16 : D / 8;
     constexpr int LPR = D / 8, RPP = NT / LPR, NP = (32 + RPP - 1) / RPP;   // rows a pass, passes a tile
@@ -251,7 +251,7 @@ template <bool BF16, int D>
 hipError_t chunk_d(const CacheArgs &a, const ChunkShape &c, hipStream_t st)
 {
     const Tiling t = make_tiling(a, c.tm);
-    const dim3 grid((unsigned)t.units, a.kv_heads * c.split);
+    const dim3 grid((unsigned)(t.units * a.kv_heads * c.split));
     switch ((t.tm * c.gs + 31) / 32) {
     case 1: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 1>), grid, dim3(64), 0, st, a, t, c.split, c.gs); break;
     case 2: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 2>), grid, dim3(128), 0, st, a, t, c.split, c.gs); break;
