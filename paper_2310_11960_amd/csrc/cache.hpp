@@ -113,13 +113,21 @@ __device__ inline CacheGroup cache_group(int heads)
 inline int token_tile(const CacheArgs &a) { return a.max_chunk < a.rows ? a.max_chunk : a.rows; }
 inline int keys_tile(const ChunkShape &c) { return 32 / c.gs; }
 
+// Runs of kScan aligned blocks that a chunk's complete blocks can touch.
+constexpr int kScan = 64;   // lanes of a wave
+inline int scan_runs(const CacheArgs &a)
+{
+    const int most = (a.max_chunk < a.rows ? a.max_chunk : a.rows) / a.r + 1;
+    return (most + kScan - 1) / kScan + 1;
+}
+
 // Threads of a launch stay below 2^32.
 inline bool cache_launches_fit(const CacheArgs &a, bool appends, bool attends, int cus)
 {
     auto fits = [&](int tm, long long heads, int threads) {
         return make_tiling(a, tm).units <= 0xffffffffLL / threads / heads;
     };
-    if (appends && !fits(a.r, a.kv_heads, 256)) return false;
+    if (appends && (!fits(a.r, a.kv_heads, 256) || (long long)a.S * scan_runs(a) >= 1 << 24)) return false;
     if (!attends) return true;
     const ChunkShape c = chunk_shape(a);
     switch (cache_route(a, cus)) {
@@ -205,12 +213,15 @@ __device__ inline bool find_tile(const CacheArgs &a, const Tiling &t, unsigned u
     const int b = tile / t.tpb, lo = b * a.r + (tile - b * t.tpb) * t.tm;
     int hi = lo + t.tm < (b + 1) * a.r ? lo + t.tm : (b + 1) * a.r;
     if (hi > s + len) hi = s + len;
-    x.pos = lo > s ? lo : s;
-    x.n = hi - x.pos;
-    x.row = c0 + x.pos - s;
-    x.start = s;
-    x.end = s + len;
-    x.row0 = c0;
+    // (uniform, whichever way it was found: scalar registers for all that follows)
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    x.seq = uniform(x.seq);
+    x.pos = uniform(lo > s ? lo : s);
+    x.n = uniform(hi) - x.pos;
+    x.start = uniform(s);
+    x.end = uniform(s + len);
+    x.row0 = uniform(c0);
+    x.row = x.row0 + x.pos - x.start;
     return true;
 }
 

@@ -146,12 +146,11 @@ __global__ __launch_bounds__(64 * NW) void cache_attend_kernel(CacheArgs a, Tili
             }
         }
         // causal: rows up to the query's own position; the far list is the past
-        const int last = i < near ? qpos - klo - 32 * i : 31;
+        const uint32_t see = seen_rows(vm, i < near ? qpos - klo - 32 * i : 31, hh);
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const int row = grow(j, hh);
-            s[j] = row <= last && (vm >> row & 1u) ? s[j] * a.scale_log2 : -INFINITY;
+            s[j] = seen(see, j) ? s[j] * a.scale_log2 : -INFINITY;
             mx = fmaxf(mx, s[j]);
         }
         const float mnew = fmaxf(m, pair_max(mx));

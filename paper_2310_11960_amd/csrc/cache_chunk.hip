@@ -3,35 +3,78 @@
 //
 // A workgroup's waves take 32 query rows each (positions times the query heads of
 // one key head) and meet every 32-row tile of keys in LDS: the previous and the
-// own block's tokens, whole rows from their pages or the caller's tensors, then
-// the far list.  The next tile's rows are in registers while one is used.
-// Products and softmax as in cache_attend.hip, with the running maximum of each
-// query; a wave leaves out the tiles behind its last query.
+// own block's tokens, which stream through two stages by direct-to-LDS loads
+// a tile ahead, then the far list, loaded once at the start.  A wave leaves
+// out the tiles behind its last query.  Per tile:
+//   S^T = K Q^T (row reads), P = exp2(c s - m), l += the sum of P,
+//   O^T += V^T P^T (bf16: transposing reads)
+// on v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32.  m follows a query's
+// maximum when that passes it by 2^8: a smaller lead only scales P, which rounds
+// to bf16 alike at any scale, and l adds the rounded P, so that a dominating
+// source still weighs exactly 1.
 //
-// What bounds it: per 32 x 32 piece the exponentials and conversions cost as many
-// cycles as the matrix products (256 + ~350 at d = 64), and a query of a block of
-// 128 meets 6 .. 9 tiles, so bytes and arithmetic weigh about the same.
+// What bounds it: issue.  A 32 x 32 piece at d = 64 takes 256 cycles of matrix
+// products and about 450 of vector work, the exponentials 256 of them; row
+// addresses per lane and a maximum per tile made it 1500 (26 us a workgroup).
 #include "cache_device.hpp"
+#include "row_groups.hpp"
 #include "wave_ops.hpp"
 
 namespace fma_dev {
 
 namespace {
 
+constexpr int kStages = 2;   // near tiles in LDS
+
+// A row's 16-byte chunk c lies at chunk c ^ chunk_swz(row).
 template <bool BF16, int D>
-struct ChunkSmem {
-    static constexpr int P = BF16 ? 2 * D : 4 * D + 16;   // row pitch (fp32: off the banks of a 256-byte stride)
-    __attribute__((aligned(16))) char k[2][32 * P], v[2][32 * P];
-    uint32_t ok[2][32];   // the row is there
+__device__ inline int chunk_swz(int row)
+{
+    if constexpr (BF16) return swzd<D>(row);
+    else return row & (D == 32 ? 7 : 15);
+}
+
+// Rows of a block's tokens: position p of [lo, hi) at k + (p - first) * sk, v likewise.
+template <bool BF16>
+struct NearRows {
+    const char *k, *v;
+    long long sk, sv;   // bytes
+    int first, lo, hi;
+    bool paged;
+    __device__ NearRows() {}
+    __device__ NearRows(const CacheArgs &a, const Tile &x, int h, int page, int first_, int end)
+    {
+        first = first_;
+        hi = end;
+        paged = page >= 0;
+        if (paged) {
+            const long long off = page_row(a, page, h, 0);
+            k = static_cast<const char *>(elem<BF16>(const_cast<const void *>(a.kp), off));
+            v = static_cast<const char *>(elem<BF16>(const_cast<const void *>(a.vp), off));
+            sk = sv = a.head_dim * (BF16 ? 2 : 4);
+            lo = first;
+        } else {   // the caller's tensors, for the new ones
+            const long long n = x.row0 + first - x.start;
+            k = static_cast<const char *>(elem<BF16>(a.k, n * a.kt + h * a.kh));
+            v = static_cast<const char *>(elem<BF16>(a.v, n * a.vt + h * a.vh));
+            sk = a.kt * (BF16 ? 2 : 4);
+            sv = a.vt * (BF16 ? 2 : 4);
+            lo = !a.k ? end : first > x.start ? first : x.start;
+        }
+    }
 };
 
 template <bool BF16, int D, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 ? 1 : D == 128 ? 2 : 3))) void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs)
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 ? 1 : D == 128 ? 2 : 4)))
+void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs, int far_cap)
 {
-    constexpr int NT = 64 * NW, ND = D / 32, NC = BF16 ? D / 16 : D / 8;
-    constexpr int LPR = D / 8, RPP = NT / LPR, NP = (32 + RPP - 1) / RPP;   // rows a pass, passes a tile
-    constexpr int P = ChunkSmem<BF16, D>::P;
-    __shared__ ChunkSmem<BF16, D> sm;
+    constexpr int ND = D / 32, NC = BF16 ? D / 16 : D / 8, RB = D * (BF16 ? 2 : 4), TB = 32 * RB;   // row, tile bytes
+    constexpr int CPR = RB / 16, RPL = 64 / CPR, NLD = TB / 1024;   // 16-byte chunks of a row, rows of a load, loads
+    constexpr int ML = (2 * NLD + NW - 1) / NW, FL = 2 * NLD / NW;  // a wave's loads of a tile, at most and at least
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    char *const ring = smem;                                        // [kStages][2][TB]
+    char *const far_k = smem + kStages * 2 * TB, *const far_v = far_k + far_cap * RB;
+    uint32_t *const far_ok = reinterpret_cast<uint32_t *>(far_v + far_cap * RB);
     Tile x;
     const CacheGroup g = cache_group(a.kv_heads * split);
     if (!find_tile(a, t, g.unit, x)) return;
@@ -39,96 +82,120 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = g.head / split, g0 = (g.head - h * split) * gs;
     const int ng = gs < a.group - g0 ? gs : a.group - g0;
-    const int b = x.pos / a.r, pos_b = b * a.r;
-    const int page = page_of(a, x.seq, b), page0 = b > 0 ? page_of(a, x.seq, b - 1) : -1;
-    const int klo = b > 0 ? pos_b - a.r : 0, kend = x.pos + x.n;
+    const int b = x.pos / a.r, pos_b = b * a.r, klo = b > 0 ? pos_b - a.r : 0, kend = x.pos + x.n;
     const int near = (kend - klo + 31) / 32;
     const FarList list(a, b);
-    const int tiles = near + (list.n + 31) / 32;
+    const NearRows<BF16> prev(a, x, h, b > 0 ? page_of(a, x.seq, b - 1) : -1, klo, pos_b);
+    const NearRows<BF16> own(a, x, h, page_of(a, x.seq, b), pos_b, kend);
 
-    // tile i's rows into registers (fp32 far rows as they are), then to LDS
-    const int lr = tid / LPR, lc = tid % LPR;
-    Raw8<BF16> rk[NP], rv[NP];
-    bool there[NP];
-    auto fetch = [&](int i) {
+    // near tile i to stage st: load j of the tile (keys, then values) by wave j % NW
+    const int lrow = lane / CPR, lchunk = lane % CPR;
+    const char *const any = static_cast<const char *>(elem<BF16>(a.q, (long long)x.row * a.qt + (h * a.group + g0) * a.qh));
+    auto issue = [&](int i, int st) __attribute__((always_inline)) {
+        const int k0 = klo + 32 * i;
+        const bool whole = k0 >= pos_b;   // (blocks of a multiple of 32: tiles do not cross them)
+        const char *const sk = whole ? own.k : prev.k, *const sv = whole ? own.v : prev.v;
+        const int first = whole ? own.first : prev.first;
+        const bool plain = (a.r & 31) == 0 && (whole ? own.paged && k0 + 32 <= own.hi : prev.paged);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const int row = lr + p * RPP;
-            rk[p] = Raw8<BF16>();
-            rv[p] = Raw8<BF16>();
-            there[p] = false;
-            if (NP * RPP > 32 && row >= 32) continue;
-            if (i < near) {
-                const int pos = klo + 32 * i + row;
-                if (pos >= kend) continue;
-                if (a.k && pos >= x.start) {
-                    const long long n = x.row0 + pos - x.start;
-                    rk[p] = load_raw<BF16>(elem<BF16>(a.k, n * a.kt + h * a.kh + 8 * lc));
-                    rv[p] = load_raw<BF16>(elem<BF16>(a.v, n * a.vt + h * a.vh + 8 * lc));
-                    there[p] = true;
-                } else {
-                    const int pg = pos >= pos_b ? page : page0;
-                    if (pg < 0) continue;
-                    const long long off = page_row(a, pg, h, pos >= pos_b ? pos - pos_b : pos - klo) + 8 * lc;
-                    rk[p] = load_raw<BF16>(elem<BF16>(const_cast<const void *>(a.kp), off));
-                    rv[p] = load_raw<BF16>(elem<BF16>(const_cast<const void *>(a.vp), off));
-                    there[p] = true;
+        for (int jj = 0; jj < ML; ++jj) {
+            const int j = wave + NW * jj;
+            if (ML != FL && j >= 2 * NLD) break;
+            const int val = j >= NLD, row = (j - val * NLD) * RPL + lrow, ch = 16 * (lchunk ^ chunk_swz<BF16, D>(row));
+            const char *p;
+            if (plain) {
+                p = (val ? sv : sk) + (k0 - first) * RB + (row * RB + ch);
+            } else {
+                // a row that is not there repeats one that is (its weight is 0, and
+                // what the page holds in its place is no number to multiply)
+                bool o = k0 + row >= pos_b;
+                o = (o ? own.lo < own.hi : prev.lo < prev.hi) ? o : !o;
+                const int lo = o ? own.lo : prev.lo, hi = o ? own.hi : prev.hi;
+                const int pos = k0 + row < lo ? lo : k0 + row >= hi ? hi - 1 : k0 + row;
+                const long long step = val ? (o ? own.sv : prev.sv) : (o ? own.sk : prev.sk);
+                p = (val ? (o ? own.v : prev.v) : (o ? own.k : prev.k)) + (pos - (o ? own.first : prev.first)) * step;
+                p = (lo < hi ? p : any) + ch;
+            }
+            dma16(p, lds_u32(ring + (2 * st + val) * TB) + (j - val * NLD) * 1024);
+        }
+    };
+    // which rows of near tile i are there
+    auto rows_there = [&](int i) {
+        const int k0 = klo + 32 * i;
+        auto bits = [&](int lo, int hi) {
+            lo = lo - k0 < 0 ? 0 : lo - k0;
+            hi = hi - k0 > 32 ? 32 : hi - k0;
+            return lo >= hi ? 0u : (hi - lo == 32 ? ~0u : ((1u << (hi - lo)) - 1) << lo);
+        };
+        return bits(prev.lo, prev.hi) | bits(own.lo, own.hi);
+    };
+    // far rows first .. of the list, fp32, to LDS in the cache's type (bf16: rounded, as
+    // the dense path keeps them); whole tiles, rows beyond the list as missing ones
+    auto far_rows = [&](int first) {
+        constexpr int LPR = D / 8, RPP = 64 * NW / LPR, U = 2;   // U passes' pages, then their rows
+        const int left = (list.n - first + 31) / 32 * 32, rows = left < far_cap ? left : far_cap, lc = tid % LPR;
+        for (int row0 = tid / LPR; row0 < rows; row0 += U * RPP) {
+            const float *far[U];
+            f32x4 f[U][2][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) far[u] = row0 + u * RPP < rows ? list.row(a, x.seq, h, first + row0 + u * RPP) : nullptr;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f[u][k >> 1][k & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (far[u]) f[u][k >> 1][k & 1] = *reinterpret_cast<const f32x4 *>(far[u] + (k >> 1) * a.sets * D + 8 * lc + 4 * (k & 1));
                 }
-            } else {
-                const float *far = list.row(a, x.seq, h, 32 * (i - near) + row);
-                if (!far) continue;
-                float f[8];
-                load8f<false>(far + 8 * lc, f);
-                rk[p] = rounded<BF16>(f);
-                load8f<false>(far + (long long)a.sets * D + 8 * lc, f);
-                rv[p] = rounded<BF16>(f);
-                there[p] = true;
             }
-        }
-    };
-    auto stage = [&](int st) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const int row = lr + p * RPP;
-            if (NP * RPP > 32 && row >= 32) continue;
-            if constexpr (BF16) {
-                const int o = row * P + 16 * (lc ^ swzd<D>(row));
-                *reinterpret_cast<uint4 *>(sm.k[st] + o) = make_uint4(rk[p].w[0], rk[p].w[1], rk[p].w[2], rk[p].w[3]);
-                *reinterpret_cast<uint4 *>(sm.v[st] + o) = make_uint4(rv[p].w[0], rv[p].w[1], rv[p].w[2], rv[p].w[3]);
-            } else {
-                float f[8];
-                f32x4 *to = reinterpret_cast<f32x4 *>(sm.k[st] + row * P + 32 * lc);
-                floats<BF16>(rk[p], f);
-                to[0] = f32x4{f[0], f[1], f[2], f[3]};
-                to[1] = f32x4{f[4], f[5], f[6], f[7]};
-                to = reinterpret_cast<f32x4 *>(sm.v[st] + row * P + 32 * lc);
-                floats<BF16>(rv[p], f);
-                to[0] = f32x4{f[0], f[1], f[2], f[3]};
-                to[1] = f32x4{f[4], f[5], f[6], f[7]};
+            for (int u = 0; u < U; ++u) {
+                const int row = row0 + u * RPP, sw = chunk_swz<BF16, D>(row);
+                if (row >= rows) continue;
+                if (lc == 0) far_ok[row] = far[u] != nullptr;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    char *const to = (kv ? far_v : far_k) + row * RB;
+                    const f32x4 lo = f[u][kv][0], hi = f[u][kv][1];
+                    if constexpr (BF16) {
+                        *reinterpret_cast<uint4 *>(to + 16 * (lc ^ sw)) = make_uint4(pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]),
+                                                                                   pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3]));
+                    } else {
+                        *reinterpret_cast<f32x4 *>(to + 16 * ((2 * lc) ^ sw)) = lo;
+                        *reinterpret_cast<f32x4 *>(to + 16 * ((2 * lc + 1) ^ sw)) = hi;
+                    }
+                }
             }
-            if (lc == 0) sm.ok[st][row] = there[p];
         }
     };
-    fetch(0);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i)
+        if (i < near) issue(i, i);
 
-    // this lane's query
+    // this lane's query; a negative scale turns its sign, so that the greatest
+    // product is the greatest score
     const int rows = x.n * ng, row = 32 * wave + l32, qi = row < rows ? row / ng : 0, gi = row < rows ? row - qi * ng : 0;
     const int qpos = x.pos + qi;
     const int wfirst = x.pos + 32 * wave / ng;   // positions of the wave's first and last rows
     const int wtop = 32 * wave + 31 < rows ? 32 * wave + 31 : rows - 1, wlast = x.pos + wtop / ng;
     const bool active = 32 * wave < rows;
+    const float scale = fabsf(a.scale_log2);
     uint4 qo[NC];
     {
         const char *p = static_cast<const char *>(elem<BF16>(a.q, (long long)(x.row + qi) * a.qt + (h * a.group + g0 + gi) * a.qh)) + 16 * hh;
+        const uint32_t sign = a.scale_log2 < 0.f ? (BF16 ? 0x80008000u : 0x80000000u) : 0u;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) qo[c] = *reinterpret_cast<const uint4 *>(p + 32 * c);
+        for (int c = 0; c < NC; ++c) {
+            qo[c] = *reinterpret_cast<const uint4 *>(p + 32 * c);
+            qo[c].x ^= sign, qo[c].y ^= sign, qo[c].z ^= sign, qo[c].w ^= sign;
+        }
     }
+    if (list.n) far_rows(0);
 
     f32x16 o[ND];
 #pragma unroll
     for (int db = 0; db < ND; ++db) o[db] = f32x16{0};
     float m = -INFINITY, l = 0.f;
-    const int koff = l32 * P + 16 * (hh ^ (BF16 ? swzd<D>(l32) : 0));
+    const int koff = l32 * RB + 16 * (hh ^ chunk_swz<BF16, D>(l32));
     int voff[2];
     {
         const int gq = lane >> 4, s4 = lane & 15, jr = s4 >> 2, qq = s4 & 3;
@@ -138,87 +205,112 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 
             voff[k] = r * D + 8 * ((2 * (gq & 1) + (qq >> 1)) ^ swzd<D>(r)) + 4 * (qq & 1);
         }
     }
-    stage(0);
+    const int tiles = near + (list.n + 31) / 32;
+#pragma unroll 1
     for (int i = 0; i < tiles; ++i) {
-        const int st = i & 1;
-        __syncthreads();
-        if (i + 1 < tiles) fetch(i + 1);
-        const int k0 = klo + 32 * i;   // (near) position of the tile's first row
-        if (active && (i >= near || k0 <= wlast)) {
-            const uint32_t vm = (uint32_t)__builtin_amdgcn_ballot_w64(sm.ok[st][l32] != 0);
-            f32x16 s = {0};
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if constexpr (BF16) {
-                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(sm.k[st] + (koff ^ (32 * c)));
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, qo[c]), s, 0, 0, 0);
-                } else {
-                    const f32x4 kf = *reinterpret_cast<const f32x4 *>(sm.k[st] + koff + 32 * c);
-                    const f32x4 qf = __builtin_bit_cast(f32x4, qo[c]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j], qf[j], s, 0, 0, 0);
-                }
+        const char *kt, *vt;
+        uint32_t vm;
+        int last;       // rows of the tile that lie behind this lane's query start there
+        bool all;       // every query of the wave sees every row
+        if (i < near) {
+            const int st = i % kStages, k0 = klo + 32 * i;
+            if (i + kStages - 2 < near)   // the tiles behind this one may be on their way
+                wait_vm<(kStages - 2) * FL>();
+            else
+                wait_vm<0>();
+            __syncthreads();
+            if (i + kStages - 1 < near) issue(i + kStages - 1, (i + kStages - 1) % kStages);
+            vm = rows_there(i);
+            if (!active || k0 > wlast || vm == 0) continue;
+            kt = ring + 2 * st * TB;
+            vt = kt + TB;
+            last = qpos - k0;
+            all = vm == ~0u && k0 + 31 <= wfirst;
+        } else {
+            const int f = 32 * (i - near), at = f % far_cap;
+            if (f > 0 && at == 0) {   // (more far rows than LDS holds)
+                __syncthreads();
+                far_rows(f);
+                __syncthreads();
             }
-            float mx = -INFINITY;
-            if (vm == 0xffffffffu && (i >= near || k0 + 31 <= wfirst)) {
+            if (!active) continue;
+            vm = (uint32_t)__builtin_amdgcn_ballot_w64(far_ok[at + l32] != 0);
+            if (vm == 0) continue;
+            kt = far_k + at * RB;
+            vt = far_v + at * RB;
+            last = 31;
+            all = vm == ~0u;
+        }
+        f32x16 s = {0};
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    s[j] *= a.scale_log2;
-                    mx = fmaxf(mx, s[j]);
-                }
+        for (int c = 0; c < NC; ++c) {
+            if constexpr (BF16) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + (koff ^ (32 * c)));
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, qo[c]), s, 0, 0, 0);
             } else {
-                const int last = i < near ? qpos - k0 : 31;
+                const f32x4 kf = *reinterpret_cast<const f32x4 *>(kt + (koff ^ (32 * c)));
+                const f32x4 qf = __builtin_bit_cast(f32x4, qo[c]);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int r = grow(j, hh);
-                    s[j] = r <= last && (vm >> r & 1u) ? s[j] * a.scale_log2 : -INFINITY;
-                    mx = fmaxf(mx, s[j]);
+                for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j], qf[j], s, 0, 0, 0);
+            }
+        }
+        if (!all) {
+            const uint32_t see = seen_rows(vm, last, hh);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[j] = seen(see, j) ? s[j] : -INFINITY;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) mx = __builtin_elementwise_maximum(mx, s[j]);
+        mx = pair_max(mx) * scale;
+        const bool up = mx > m + 8.f || m == -INFINITY;
+        if (__builtin_amdgcn_ballot_w64(up) != 0) {
+            const float mnew = up ? mx : m;
+            const float corr = mnew == m ? 1.f : __builtin_amdgcn_exp2f(m - mnew);   // (-inf: still nothing seen)
+            m = mnew;
+            l *= corr;
+#pragma unroll
+            for (int db = 0; db < ND; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[db][j] *= corr;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale, -ref));
+        if constexpr (BF16) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            const bf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    w[k] = pack_bf16(s[8 * hf + 2 * k], s[8 * hf + 2 * k + 1]);
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[k]), ones, l, false);
+                }
+                const uint4 pw = make_uint4(w[0], w[1], w[2], w[3]);
+                const __bf16 *const v16 = reinterpret_cast<const __bf16 *>(vt) + 16 * hf * D;
+#pragma unroll
+                for (int db = 0; db < ND; ++db) {
+                    const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v16 + (voff[0] ^ (32 * db))));
+                    const s16x4 r2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v16 + (voff[1] ^ (32 * db))));
+                    const s16x8 av = {r1[0], r1[1], r1[2], r1[3], r2[0], r2[1], r2[2], r2[3]};
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av),
+                                                                    __builtin_bit_cast(bf16x8, pw), o[db], 0, 0, 0);
                 }
             }
-            mx = pair_max(mx);
-            if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
-                const float mnew = fmaxf(m, mx);
-                const float corr = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mnew);
-                m = mnew;
-                l *= corr;
-#pragma unroll
-                for (int db = 0; db < ND; ++db)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[db][j] *= corr;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;   // a query that has seen nothing yet
+        } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                s[j] = __builtin_amdgcn_exp2f(s[j] - ref);
                 l += s[j];
-            }
-            if constexpr (BF16) {
+                const int r = grow(j, hh), sw = chunk_swz<BF16, D>(r);
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    const uint4 pw = make_uint4(pack_bf16(s[8 * hf], s[8 * hf + 1]), pack_bf16(s[8 * hf + 2], s[8 * hf + 3]),
-                                                pack_bf16(s[8 * hf + 4], s[8 * hf + 5]),
-                                                pack_bf16(s[8 * hf + 6], s[8 * hf + 7]));
-                    const __bf16 *vt = reinterpret_cast<const __bf16 *>(sm.v[st]) + 16 * hf * D;
-#pragma unroll
-                    for (int db = 0; db < ND; ++db) {
-                        const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + (voff[0] ^ (32 * db))));
-                        const s16x4 r2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vt + (voff[1] ^ (32 * db))));
-                        const s16x8 av = {r1[0], r1[1], r1[2], r1[3], r2[0], r2[1], r2[2], r2[3]};
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av),
-                                                                        __builtin_bit_cast(bf16x8, pw), o[db], 0, 0, 0);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float *vr = reinterpret_cast<const float *>(sm.v[st] + grow(j, hh) * P) + l32;
-#pragma unroll
-                    for (int db = 0; db < ND; ++db)
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vr[32 * db], s[j], o[db], 0, 0, 0);
+                for (int db = 0; db < ND; ++db) {
+                    const float vf = *reinterpret_cast<const float *>(vt + r * RB + 16 * ((8 * db + (l32 >> 2)) ^ sw) + 4 * (l32 & 3));
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[j], o[db], 0, 0, 0);
                 }
             }
         }
-        if (i + 1 < tiles) stage(st ^ 1);
     }
     if (!active) return;
     l = pair_sum(l);
@@ -247,18 +339,34 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 
     }
 }
 
+template <bool BF16, int D, int NW>
+hipError_t chunk_w(const CacheArgs &a, const ChunkShape &c, const Tiling &t, hipStream_t st)
+{
+    constexpr int RB = D * (BF16 ? 2 : 4);
+    int far = (2 * a.sets + 31) / 32 * 32;   // the longest list
+    constexpr int kMost = RB == 512 ? 32 : 64;   // at a time, within 160 KB
+    if (far > kMost) far = kMost;
+    const int lds = kStages * 2 * 32 * RB + far * (2 * RB + 4);
+    if (lds > 65536) {
+        const void *const fn = reinterpret_cast<const void *>(cache_chunk_kernel<BF16, D, NW>);
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, NW>), dim3((unsigned)(t.units * a.kv_heads * c.split)), dim3(64 * NW), lds,
+                       st, a, t, c.split, c.gs, far);
+    return hipGetLastError();
+}
+
 template <bool BF16, int D>
 hipError_t chunk_d(const CacheArgs &a, const ChunkShape &c, hipStream_t st)
 {
     const Tiling t = make_tiling(a, c.tm);
-    const dim3 grid((unsigned)(t.units * a.kv_heads * c.split));
     switch ((t.tm * c.gs + 31) / 32) {
-    case 1: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 1>), grid, dim3(64), 0, st, a, t, c.split, c.gs); break;
-    case 2: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 2>), grid, dim3(128), 0, st, a, t, c.split, c.gs); break;
-    case 3: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 3>), grid, dim3(192), 0, st, a, t, c.split, c.gs); break;
-    default: hipLaunchKernelGGL((cache_chunk_kernel<BF16, D, 4>), grid, dim3(256), 0, st, a, t, c.split, c.gs); break;
+    case 1: return chunk_w<BF16, D, 1>(a, c, t, st);
+    case 2: return chunk_w<BF16, D, 2>(a, c, t, st);
+    case 3: return chunk_w<BF16, D, 3>(a, c, t, st);
+    default: return chunk_w<BF16, D, 4>(a, c, t, st);
     }
-    return hipGetLastError();
 }
 
 }  // namespace

@@ -33,6 +33,16 @@ __device__ inline void load8f(const void *p, float (&x)[8])
     floats<BF16>(load_raw<BF16>(p), x);
 }
 
+// Rows 0 .. 31 of a tile that a lane's query sees, as bits: those of `there` up to
+// row `last`; shifted so that accumulator element j of lane half hh is bit
+// 8 (j >> 2) + (j & 3).
+__device__ inline uint32_t seen_rows(uint32_t there, int last, int hh)
+{
+    const uint32_t upto = last >= 31 ? ~0u : last < 0 ? 0u : (2u << last) - 1;
+    return (there & upto) >> (4 * hh);
+}
+__device__ inline bool seen(uint32_t rows, int j) { return rows >> (8 * (j >> 2) + (j & 3)) & 1u; }
+
 // The far field of queries in block b: level by level group q - 2 and (odd q)
 // group q - 3, each with all bases; groups that a finer level covers and
 // empty levels take no place in the list.
