@@ -87,13 +87,38 @@ __global__ __launch_bounds__(kThreads) void cache_blocks_kernel(CacheArgs a, Til
 // Pass 2: a thread per channel of a set walks the blocks that the call completed,
 // kScan of them on their way at a time (a wave's block is uniform).  Runs of
 // kScan blocks that start at a multiple of kScan hold whole groups of up to kScan
-// blocks and go to workgroups of their own; the levels above are walked from run
-// to run by the first of them.
+// blocks and go to workgroups of their own.  Groups of more blocks (tall ones):
+//   SCAN_ALL     the first run's workgroup walks on through the others;
+//   or, for chunks of several runs,
+//   SCAN_TOTALS  every run that another follows leaves its total in its last
+//                block's row,
+//   SCAN_CHAIN   one thread per channel makes these the sums at the runs' ends,
+//   SCAN_RUNS    every run starts from the sum at the end of the one before.
 // Two prompts of 98K tokens together, 16 heads: 93 us with 16 blocks on their
-// way, 53 with 64, XX with the runs apart.
+// way, 53 with 64, 59 with the runs apart and tall groups walked, 39 in three steps.
+enum ScanStep { SCAN_ALL, SCAN_TOTALS, SCAN_CHAIN, SCAN_RUNS };
+
+// blocks b .. b + n - 1 of a channel on their way: mine, lane i's page of block b + i
+__device__ __attribute__((always_inline)) inline void scan_fetch(const float *base, long long page, int col, int mine, int n,
+                                                                 bool live, float (&own)[kScan])
+{
+#pragma unroll
+    for (int i = 0; i < kScan; i += 8) {
+        if (i < n) {
+#pragma unroll
+            for (int k = i; k < i + 8; ++k) {
+                const int p = __builtin_amdgcn_readlane(mine, k);
+                own[k] = p >= 0 && live ? (base + p * page)[col] : 0.f;
+            }
+        }
+    }
+}
+
+template <int STEP>
 __global__ __launch_bounds__(kThreads) void cache_scan_kernel(CacheArgs a, int runs)
 {
-    const int seq = blockIdx.x / (unsigned)runs, run = blockIdx.x - seq * runs, h = blockIdx.y, lane = threadIdx.x & 63;
+    const int per = STEP == SCAN_CHAIN ? 1 : runs;   // workgroups along a sequence
+    const int seq = blockIdx.x / (unsigned)per, run = blockIdx.x - seq * per, h = blockIdx.y, lane = threadIdx.x & 63;
     const int cols = 2 * a.sets * a.head_dim, at = blockIdx.z * kThreads + threadIdx.x;
     const int col = at < cols ? at : 0;   // (whole waves stay: every lane holds a block's page)
     const int c0 = listed(a.cu, seq), c1 = listed(a.cu, seq + 1), s = listed(a.start, seq);
@@ -101,37 +126,92 @@ __global__ __launch_bounds__(kThreads) void cache_scan_kernel(CacheArgs a, int r
     const int l = col / a.head_dim % a.sets / a.rank;
     const int first = s / a.r, b1 = (s + c1 - c0) / a.r, run0 = (first / kScan + run) * kScan;
     const bool tall = (1 << l) > kScan;
-    bool live = at < cols && l > 0 && (!tall || run == 0);   // a group of level 1 is one block
+    bool live = at < cols && l > 0;   // a group of level 1 is one block
     float *const base = a.sum + (long long)h * cols;
     const long long page = (long long)a.kv_heads * cols;
-    float acc = 0.f;
-    if (run == 0 && first > 0) {
-        const int prev = summary_of(a, seq, first - 1);
-        if (prev >= 0) acc = (base + prev * page)[col];
+    auto sum_at = [&](int b) {
+        const int p = b >= 0 ? summary_of(a, seq, b) : -1;
+        return p >= 0 ? (base + p * page)[col] : 0.f;
+    };
+    float own[kScan];
+    if constexpr (STEP == SCAN_CHAIN) {
+        live = live && tall;
+        if (__builtin_amdgcn_ballot_w64(live) == 0) return;
+        // the ends of the runs that others follow, kScan at a time
+        float acc = 0.f;
+        for (int e = run0 + kScan - 1; e < b1 - 1; e += kScan * kScan) {
+            const int end = e + lane * kScan, mine = end < b1 - 1 ? summary_of(a, seq, end) : -1;
+            const int n = (b1 - 2 - e) / kScan + 1 < kScan ? (b1 - 2 - e) / kScan + 1 : kScan;
+            scan_fetch(base, page, col, mine, n, live, own);
+#pragma unroll
+            for (int i = 0; i < kScan; i += 8) {
+                if (i < n) {
+#pragma unroll
+                    for (int k = i; k < i + 8; ++k) {
+                        if (k >= n) continue;
+                        const int p = __builtin_amdgcn_readlane(mine, k);
+                        // (the run of end e + k kScan starts a group, or goes on with one)
+                        acc = (e + (k - 1) * kScan + 1) & ((1 << l) - 1) ? acc + own[k] : own[k];
+                        if (p < 0)
+                            acc = 0.f;
+                        else if (live)
+                            (base + p * page)[col] = acc;
+                    }
+                }
+            }
+        }
+        return;
     }
-    for (int b = run == 0 ? first : run0; b < b1;) {
+    int b = run == 0 ? first : run0;
+    if (b >= b1) return;
+    if constexpr (STEP == SCAN_TOTALS) live = live && tall && b / kScan * kScan + kScan < b1;
+    if constexpr (STEP == SCAN_ALL) live = live && (!tall || run == 0);
+    if (__builtin_amdgcn_ballot_w64(live) == 0) return;
+    // the sum before the piece, where a group goes on through its start
+    float acc = live && (b & ((1 << l) - 1)) && (run == 0 || STEP == SCAN_RUNS) ? sum_at(b - 1) : 0.f;
+    while (b < b1) {
         const int end = b / kScan * kScan + kScan;   // the walk's pieces end with the runs
         const int n = (end < b1 ? end : b1) - b;
-        const int mine = lane < n ? summary_of(a, seq, b + lane) : -1;   // lane i: page of block b + i
-        float own[kScan];
+        const int mine = lane < n ? summary_of(a, seq, b + lane) : -1;
+        const int keep = STEP == SCAN_RUNS && tall && end < b1 ? n - 1 : n;   // (a run's end is there already)
+        scan_fetch(base, page, col, mine, n, live, own);
 #pragma unroll
-        for (int i = 0; i < kScan; ++i) {
-            own[i] = 0.f;
-            const int p = __builtin_amdgcn_readlane(mine, i);
-            if (p >= 0 && live) own[i] = (base + p * page)[col];
-        }
+        for (int i = 0; i < kScan; i += 8) {
+            if (i < n) {
 #pragma unroll
-        for (int i = 0; i < kScan; ++i) {
-            const int p = __builtin_amdgcn_readlane(mine, i);
-            acc = (b + i) & ((1 << l) - 1) ? acc + own[i] : own[i];
-            if (p < 0)
-                acc = 0.f;   // the sums of a missing page count as zero (and none follows the last block)
-            else if (live)
-                (base + p * page)[col] = acc;
+                for (int k = i; k < i + 8; ++k) {
+                    if (k >= n) continue;
+                    const int p = __builtin_amdgcn_readlane(mine, k);
+                    acc = (b + k) & ((1 << l) - 1) ? acc + own[k] : own[k];
+                    if (p < 0)
+                        acc = 0.f;   // the sums of a missing page count as zero
+                    else if (live && (STEP == SCAN_TOTALS ? k == n - 1 : k < keep))
+                        (base + p * page)[col] = acc;
+                }
+            }
         }
-        live = live && tall;
+        live = live && tall && STEP == SCAN_ALL;
         if (__builtin_amdgcn_ballot_w64(live) == 0) break;
         b = end;
+    }
+}
+
+template <int STEP>
+void launch_scan(const CacheArgs &a, int runs, hipStream_t st)
+{
+    const dim3 grid((unsigned)a.S * (STEP == SCAN_CHAIN ? 1 : runs), a.kv_heads, (2 * a.sets * a.head_dim + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL((cache_scan_kernel<STEP>), grid, dim3(kThreads), 0, st, a, runs);
+}
+
+void launch_scans(const CacheArgs &a, hipStream_t st)
+{
+    const int runs = scan_runs(a);
+    if (runs > 3 && (1 << (a.levels - 1)) > kScan) {
+        launch_scan<SCAN_TOTALS>(a, runs, st);
+        launch_scan<SCAN_CHAIN>(a, runs, st);
+        launch_scan<SCAN_RUNS>(a, runs, st);
+    } else {
+        launch_scan<SCAN_ALL>(a, runs, st);
     }
 }
 
@@ -145,9 +225,7 @@ hipError_t append_d(const CacheArgs &a, hipStream_t st)
     }
     hipLaunchKernelGGL((cache_blocks_kernel<BF16, D>), dim3((unsigned)(t.units * ((a.kv_heads + 1) / 2))), dim3(kThreads),
                        0, st, a, t);
-    if (a.levels > 1)
-        hipLaunchKernelGGL(cache_scan_kernel, dim3((unsigned)a.S * scan_runs(a), a.kv_heads, (2 * a.sets * D + kThreads - 1) / kThreads),
-                           dim3(kThreads), 0, st, a, scan_runs(a));
+    if (a.levels > 1) launch_scans(a, st);
     return hipGetLastError();
 }
 

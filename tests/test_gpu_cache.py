@@ -183,6 +183,21 @@ def test_longer_pieces_with_missing_pages(dtype):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("pieces", [(37, 100, 3), (70, 300, 1), (129, 128, 60), (1, 64, 200), (380, 1, 2)],
+                         ids=lambda p: "-".join(map(str, p)))
+def test_sums_over_many_blocks(pieces, dtype):
+    """Groups of 128 and 256 blocks whose sums cross several calls, at and away
+    from the multiples of 64 blocks where the walk over them is cut."""
+    r = 16
+    lens = [r * p + x for p, x in zip(pieces, (5, 0, -2))]
+    s = Served([sum(lens), r * 40 + 3], 2, 1, 32, r, 1, max_len=r * 512, dtype=DT[dtype], seed=14)
+    s.step([lens[0], 0], "append")
+    s.step([lens[1], r * 40], "append")
+    s.step([lens[2], 3])
+    s.check_pages()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 def test_token_by_token(dtype):
     s = Served([16 * 11 + 3, 16 * 4], 2, 1, 32, 16, 1, max_len=16 * 16, dtype=DT[dtype], seed=2)
     s.step([16 * 3 - 2, 0], "append")
