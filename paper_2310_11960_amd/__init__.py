@@ -15,6 +15,7 @@ High-level use::
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -161,14 +162,14 @@ def library() -> ctypes.CDLL:
     lib.fma_forward_static.argtypes = [vp] * 8
     lib.fma_stream_reference.argtypes = [vp, ctypes.c_size_t, vp, ctypes.c_size_t, i32, vp]
     lib.fma_plan_params.argtypes = [vp, ctypes.POINTER(i64), i32, ctypes.POINTER(i32)]
-    view = ctypes.POINTER(fma_view_t)
+    view = vp   # (structs by reference, or the addresses of some that lie together)
     lib.fma_qk_plan.argtypes = [ctypes.POINTER(fma_qk_desc_t), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(vp)]
     lib.fma_qk_destroy.argtypes = [vp]
     lib.fma_qk_norm_rope.argtypes = [vp, i32, i64, view, view, view, vp, vp, vp, view, view, view, vp]
     lib.fma_qk_backward_workspace_size.argtypes = [vp, i32, i64, ctypes.POINTER(ctypes.c_size_t)]
     lib.fma_qk_norm_rope_backward.argtypes = [vp, i32, i64, view, view, vp, vp, vp] + [view] * 6 + [
         vp, vp, vp, ctypes.c_size_t, vp]
-    batch = ctypes.POINTER(fma_cache_batch_t)
+    batch = vp
     lib.fma_cache_plan.argtypes = [ctypes.POINTER(fma_cache_desc_t), ctypes.POINTER(vp)]
     lib.fma_cache_destroy.argtypes = [vp]
     lib.fma_cache_sizes.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)]
@@ -209,8 +210,14 @@ def _ptr(t) -> int | None:
     return t.data_ptr()
 
 
+# the current stream's handle without the objects around it, where torch has such a call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -337,6 +344,11 @@ def fma_backward_linear(plan, q, k, v, wk, wv, wq, out, dout, dq, dk, dv, dwk, d
                                          _ptr(dwv), _ptr(dwq), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
+def _ref(x):
+    """A struct argument: the struct, its address or None."""
+    return x if x is None or isinstance(x, int) else ctypes.byref(x)
+
+
 def fma_qk_plan(desc: fma_qk_desc_t, inv_freq=None) -> int:
     h = ctypes.c_void_p()
     rates = None if inv_freq is None else (ctypes.c_double * len(inv_freq))(*inv_freq)
@@ -350,8 +362,8 @@ def fma_qk_destroy(plan: int) -> None:
 
 def fma_qk_norm_rope(plan, batch, tokens, q, k, v, gamma_q, gamma_k, positions, q_out, k_out, v_out, stream=None):
     """q, k, v, q_out, k_out, v_out: fma_view_t (v, v_out may be None)."""
-    _check(library().fma_qk_norm_rope(plan, batch, tokens, q, k, v, _ptr(gamma_q), _ptr(gamma_k), _ptr(positions),
-                                      q_out, k_out, v_out, _stream(stream)))
+    _check(library().fma_qk_norm_rope(plan, batch, tokens, _ref(q), _ref(k), _ref(v), _ptr(gamma_q), _ptr(gamma_k),
+                                      _ptr(positions), _ref(q_out), _ref(k_out), _ref(v_out), _stream(stream)))
 
 
 def fma_qk_backward_workspace_size(plan: int, batch: int, tokens: int) -> int:
@@ -363,9 +375,10 @@ def fma_qk_backward_workspace_size(plan: int, batch: int, tokens: int) -> int:
 def fma_qk_norm_rope_backward(plan, batch, tokens, q, k, gamma_q, gamma_k, positions, g_q, g_k, g_v, dq, dk, dv,
                               dgamma_q, dgamma_k, workspace, workspace_bytes, stream=None):
     """q, k, g_q, g_k, g_v, dq, dk, dv: fma_view_t (g_v, dv may be None)."""
-    _check(library().fma_qk_norm_rope_backward(plan, batch, tokens, q, k, _ptr(gamma_q), _ptr(gamma_k),
-                                               _ptr(positions), g_q, g_k, g_v, dq, dk, dv, _ptr(dgamma_q),
-                                               _ptr(dgamma_k), _ptr(workspace), workspace_bytes, _stream(stream)))
+    _check(library().fma_qk_norm_rope_backward(plan, batch, tokens, _ref(q), _ref(k), _ptr(gamma_q), _ptr(gamma_k),
+                                               _ptr(positions), _ref(g_q), _ref(g_k), _ref(g_v), _ref(dq), _ref(dk),
+                                               _ref(dv), _ptr(dgamma_q), _ptr(dgamma_k), _ptr(workspace),
+                                               workspace_bytes, _stream(stream)))
 
 
 def fma_cache_plan(desc: fma_cache_desc_t) -> int:
@@ -387,15 +400,16 @@ def fma_cache_sizes(plan: int) -> tuple[int, int, int]:
 
 def fma_cache_append(plan, batch, k, v, wk, wv, stream=None):
     """batch: fma_cache_batch_t; k, v: fma_view_t."""
-    _check(library().fma_cache_append(plan, batch, k, v, _ptr(wk), _ptr(wv), _stream(stream)))
+    _check(library().fma_cache_append(plan, _ref(batch), _ref(k), _ref(v), _ptr(wk), _ptr(wv), _stream(stream)))
 
 
 def fma_cache_attend(plan, batch, q, out, stream=None):
-    _check(library().fma_cache_attend(plan, batch, q, out, _stream(stream)))
+    _check(library().fma_cache_attend(plan, _ref(batch), _ref(q), _ref(out), _stream(stream)))
 
 
 def fma_cache_step(plan, batch, q, k, v, wk, wv, out, stream=None):
-    _check(library().fma_cache_step(plan, batch, q, k, v, _ptr(wk), _ptr(wv), out, _stream(stream)))
+    _check(library().fma_cache_step(plan, _ref(batch), _ref(q), _ref(k), _ref(v), _ptr(wk), _ptr(wv), _ref(out),
+                                    _stream(stream)))
 
 
 def fma_last_error() -> str:
@@ -565,29 +579,36 @@ def _refuse(status, message, *args):
     raise FmaError(status, message % args)
 
 
-def _view(t, name, shape, axes, dtype, device):
-    """fma_view_t of a tensor whose axes (batch, heads, tokens) are `axes`."""
+def _explain(t, name, shape, dtype, gpu):
+    """Raises what is wrong with a tensor."""
     if t.shape != shape:
         _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), tuple(shape))
-    if t.dtype != dtype or t.device != device:
-        _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, dtype, device)
+    if t.dtype is not dtype or t.get_device() != gpu:
+        _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on GPU %d", name, t.dtype, t.device, dtype, gpu)
+
+
+def _view(t, name, shape, axes, dtype, gpu):
+    """The fields of the fma_view_t of a tensor whose axes (batch, heads,
+    tokens) are `axes`."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != gpu:
+        _explain(t, name, shape, dtype, gpu)
     s = t.stride()
     if s[3] != 1:
         _refuse(FMA_ERR_SHAPE, "the channels of %s are not adjacent", name)
-    return fma_view_t(t.data_ptr(), s[axes[0]], s[axes[1]], s[axes[2]])
+    return t.data_ptr(), s[axes[0]], s[axes[1]], s[axes[2]]
 
 
 _TOKEN_MAJOR, _HEAD_MAJOR = (0, 2, 1), (0, 1, 2)   # [batch, tokens, heads, d], [batch, heads, tokens, d]
+_VIEW = ctypes.sizeof(fma_view_t)
+_VIEWS = {n: ctypes.c_int64 * (4 * n) for n in range(1, 9)}   # n views that lie together
 
 
-def _plain(t, name, shape, dtype, device):
+def _plain(t, name, shape, dtype, gpu):
     """A dense side input (None passes)."""
     if t is None:
         return
-    if t.dtype != dtype or t.device != device:
-        _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, dtype, device)
-    if t.shape != shape:
-        _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), tuple(shape))
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != gpu:
+        _explain(t, name, shape, dtype, gpu)
     if not t.is_contiguous():
         _refuse(FMA_ERR_SHAPE, "%s is not contiguous", name)
 
@@ -597,8 +618,6 @@ class _Launch:
     one, the stream that the call's allocations belong to."""
 
     def __init__(self, device, stream):
-        if device.type != "cuda":
-            _refuse(FMA_ERR_ARG, "tensors are on %s, expected a GPU", device)
         self.entered = []
         if device.index != torch.cuda.current_device():
             self.entered.append(torch.cuda.device(device))
@@ -616,6 +635,19 @@ class _Launch:
     def __exit__(self, *exc):
         for c in reversed(self.entered):
             c.__exit__(*exc)
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _launch(t, stream):
+    """Context of a call on t's device, which must be a GPU."""
+    gpu = t.get_device()
+    if gpu < 0:
+        _refuse(FMA_ERR_ARG, "tensors are on %s, expected a GPU", t.device)
+    if stream is None and gpu == torch.cuda.current_device():
+        return _HERE
+    return _Launch(t.device, stream)
 
 
 class QKNormRope:
@@ -653,13 +685,13 @@ class QKNormRope:
                 pass
             self.handle = None
 
-    def _side(self, dev, gamma_q, gamma_k, positions, B, n):
-        d = self.head_dim
-        _plain(gamma_q, "gamma_q", (d,), torch.float32, dev)
-        _plain(gamma_k, "gamma_k", (d,), torch.float32, dev)
+    def _side(self, gpu, gamma_q, gamma_k, positions, B, n):
+        f32, d = torch.float32, (self.head_dim,)
+        _plain(gamma_q, "gamma_q", d, f32, gpu)
+        _plain(gamma_k, "gamma_k", d, f32, gpu)
         if positions is not None and positions.dim() == 2 and self.axes == 1:
             positions = positions[..., None]
-        _plain(positions, "positions", (B, n, self.axes), torch.int32, dev)
+        _plain(positions, "positions", (B, n, self.axes), torch.int32, gpu)
         return positions
 
     def forward(self, q, k, v=None, gamma_q=None, gamma_k=None, positions=None, q_out=None, k_out=None, v_out=None,
@@ -670,23 +702,27 @@ class QKNormRope:
         ``t.transpose(1, 2)``).  positions: int32 [B, n] or [B, n, axes]."""
         if q.dim() != 4:
             _refuse(FMA_ERR_SHAPE, "q has %d axes, expected [B, n, heads, d]", q.dim())
-        B, n, dev, d = q.shape[0], q.shape[1], q.device, self.head_dim
-        with _Launch(dev, stream):
-            positions = self._side(dev, gamma_q, gamma_k, positions, B, n)
+        (B, n), gpu, d, dt = q.shape[:2], q.get_device(), self.head_dim, self.dtype
+        ins, kvs, outs, kvo = (B, n, self.heads, d), (B, n, self.kv_heads, d), (B, self.heads, n, d), (B, self.kv_out, n, d)
+        with _launch(q, stream):
+            positions = self._side(gpu, gamma_q, gamma_k, positions, B, n)
             if q_out is None:
-                q_out = torch.empty((B, self.heads, n, d), dtype=self.dtype, device=dev)
+                q_out = q.new_empty(outs)
             if k_out is None:
-                k_out = torch.empty((B, self.kv_out, n, d), dtype=self.dtype, device=dev)
-            if v is not None and v_out is None:
-                v_out = torch.empty((B, self.kv_out, n, d), dtype=self.dtype, device=dev)
-            a = (self.dtype, dev)
-            kvs, outs = (B, n, self.kv_heads, d), (B, self.kv_out, n, d)
-            fma_qk_norm_rope(
-                self.handle, B, n, _view(q, "q", (B, n, self.heads, d), _TOKEN_MAJOR, *a),
-                _view(k, "k", kvs, _TOKEN_MAJOR, *a), None if v is None else _view(v, "v", kvs, _TOKEN_MAJOR, *a),
-                gamma_q, gamma_k, positions, _view(q_out, "q_out", (B, self.heads, n, d), _HEAD_MAJOR, *a),
-                _view(k_out, "k_out", outs, _HEAD_MAJOR, *a),
-                None if v_out is None else _view(v_out, "v_out", outs, _HEAD_MAJOR, *a))
+                k_out = q.new_empty(kvo)
+            views = [*_view(q, "q", ins, _TOKEN_MAJOR, dt, gpu), *_view(k, "k", kvs, _TOKEN_MAJOR, dt, gpu),
+                     *_view(q_out, "q_out", outs, _HEAD_MAJOR, dt, gpu), *_view(k_out, "k_out", kvo, _HEAD_MAJOR, dt, gpu)]
+            if v is not None:
+                if v_out is None:
+                    v_out = q.new_empty(kvo)
+                views += _view(v, "v", kvs, _TOKEN_MAJOR, dt, gpu)
+            if v_out is not None:
+                views += _view(v_out, "v_out", kvo, _HEAD_MAJOR, dt, gpu)
+            buf = _VIEWS[len(views) // 4](*views)
+            at = ctypes.addressof(buf)
+            vi, vo = (at + 4 * _VIEW if v is not None else None), (at + (len(views) // 4 - 1) * _VIEW if v_out is not None else None)
+            fma_qk_norm_rope(self.handle, B, n, at, at + _VIEW, vi, gamma_q, gamma_k, positions, at + 2 * _VIEW,
+                             at + 3 * _VIEW, vo)
         return q_out, k_out, v_out
 
     def backward(self, q, k, gamma_q, gamma_k, g_q, g_k, g_v=None, positions=None, dq=None, dk=None, dv=None,
@@ -697,29 +733,32 @@ class QKNormRope:
         gamma of None has no gradient."""
         if q.dim() != 4:
             _refuse(FMA_ERR_SHAPE, "q has %d axes, expected [B, n, heads, d]", q.dim())
-        B, n, dev, d = q.shape[0], q.shape[1], q.device, self.head_dim
-        kvs, outs = (B, n, self.kv_heads, d), (B, self.kv_out, n, d)
-        with _Launch(dev, stream):
-            positions = self._side(dev, gamma_q, gamma_k, positions, B, n)
-            new = lambda *s: torch.empty(s, dtype=self.dtype, device=dev)  # noqa: E731
-            dq = new(B, n, self.heads, d) if dq is None else dq
-            dk = new(*kvs) if dk is None else dk
+        (B, n), gpu, d, dt = q.shape[:2], q.get_device(), self.head_dim, self.dtype
+        ins, kvs, outs, kvo = (B, n, self.heads, d), (B, n, self.kv_heads, d), (B, self.heads, n, d), (B, self.kv_out, n, d)
+        with _launch(q, stream):
+            positions = self._side(gpu, gamma_q, gamma_k, positions, B, n)
+            dq = q.new_empty(ins) if dq is None else dq
+            dk = q.new_empty(kvs) if dk is None else dk
             if g_v is not None and dv is None:
-                dv = new(*kvs)
+                dv = q.new_empty(kvs)
             dgq = None if gamma_q is None else torch.empty_like(gamma_q)
             dgk = None if gamma_k is None else torch.empty_like(gamma_k)
             need = fma_qk_backward_workspace_size(self.handle, B, n)
             if workspace is None:
-                workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
-            a = (self.dtype, dev)
-            fma_qk_norm_rope_backward(
-                self.handle, B, n, _view(q, "q", (B, n, self.heads, d), _TOKEN_MAJOR, *a),
-                _view(k, "k", kvs, _TOKEN_MAJOR, *a), gamma_q, gamma_k, positions,
-                _view(g_q, "g_q", (B, self.heads, n, d), _HEAD_MAJOR, *a), _view(g_k, "g_k", outs, _HEAD_MAJOR, *a),
-                None if g_v is None else _view(g_v, "g_v", outs, _HEAD_MAJOR, *a),
-                _view(dq, "dq", (B, n, self.heads, d), _TOKEN_MAJOR, *a), _view(dk, "dk", kvs, _TOKEN_MAJOR, *a),
-                None if dv is None else _view(dv, "dv", kvs, _TOKEN_MAJOR, *a), dgq, dgk, workspace,
-                workspace.numel() * workspace.element_size())
+                workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+            views = [*_view(q, "q", ins, _TOKEN_MAJOR, dt, gpu), *_view(k, "k", kvs, _TOKEN_MAJOR, dt, gpu),
+                     *_view(g_q, "g_q", outs, _HEAD_MAJOR, dt, gpu), *_view(g_k, "g_k", kvo, _HEAD_MAJOR, dt, gpu),
+                     *_view(dq, "dq", ins, _TOKEN_MAJOR, dt, gpu), *_view(dk, "dk", kvs, _TOKEN_MAJOR, dt, gpu)]
+            if g_v is not None:
+                views += _view(g_v, "g_v", kvo, _HEAD_MAJOR, dt, gpu)
+            if dv is not None:
+                views += _view(dv, "dv", kvs, _TOKEN_MAJOR, dt, gpu)
+            buf = _VIEWS[len(views) // 4](*views)
+            at = ctypes.addressof(buf)
+            gv, dvv = (at + 6 * _VIEW if g_v is not None else None), (at + (len(views) // 4 - 1) * _VIEW if dv is not None else None)
+            fma_qk_norm_rope_backward(self.handle, B, n, at, at + _VIEW, gamma_q, gamma_k, positions, at + 2 * _VIEW,
+                                      at + 3 * _VIEW, gv, at + 4 * _VIEW, at + 5 * _VIEW, dvv, dgq, dgk, workspace,
+                                      workspace.numel() * workspace.element_size())
         return dq, dk, dv, dgq, dgk
 
 
@@ -781,81 +820,83 @@ class FMACache:
                           torch.empty(sums, dtype=torch.float32, device=device) if self.sets else None)
 
     # ---------------------------------------------------------- helpers
-    def _batch(self, pages, batch, rows, dev):
+    def _batch(self, pages, batch, rows, gpu):
         kp, vp, sums = pages
         cu, start, table, stable, chunk = batch
-        S, i32 = start.shape[0], torch.int32
+        i32 = torch.int32
         if kp.dim() != 4 or table.dim() != 2 or start.dim() != 1:
             _refuse(FMA_ERR_SHAPE, "expected pages [n, kv_heads, block, d], tables [sequences, blocks], start [sequences]")
-        page = (kp.shape[0], self.kv_heads, self.block, self.head_dim)
-        _plain(kp, "k_pages", page, self.dtype, dev)
-        _plain(vp, "v_pages", page, self.dtype, dev)
-        _plain(cu, "cu_tokens", (S + 1,), i32, dev)
-        _plain(start, "start", (S,), i32, dev)
-        _plain(table, "page_table", (S, table.shape[1]), i32, dev)
-        nsum = 0
+        S, width, npage, nsum = start.shape[0], table.shape[1], kp.shape[0], 0
+        page = (npage, self.kv_heads, self.block, self.head_dim)
+        _plain(kp, "k_pages", page, self.dtype, gpu)
+        _plain(vp, "v_pages", page, self.dtype, gpu)
+        _plain(cu, "cu_tokens", (S + 1,), i32, gpu)
+        _plain(start, "start", (S,), i32, gpu)
+        _plain(table, "page_table", (S, width), i32, gpu)
+        at_sum = at_stable = None
         if self.sets:
             if sums is None or stable is None:
                 _refuse(FMA_ERR_NULL, "the plan's coarse sets need summaries and a summary_table")
             nsum = sums.shape[0]
-            _plain(sums, "summaries", (nsum, self.kv_heads, 2, self.sets, self.head_dim), torch.float32, dev)
-            _plain(stable, "summary_table", table.shape, i32, dev)
-        return fma_cache_batch_t(kp.data_ptr(), vp.data_ptr(), sums.data_ptr() if self.sets else None, kp.shape[0], nsum,
-                                 table.data_ptr(), stable.data_ptr() if self.sets else None, table.shape[1], cu.data_ptr(),
-                                 start.data_ptr(), S, chunk, rows)
+            _plain(sums, "summaries", (nsum, self.kv_heads, 2, self.sets, self.head_dim), torch.float32, gpu)
+            _plain(stable, "summary_table", (S, width), i32, gpu)
+            at_sum, at_stable = sums.data_ptr(), stable.data_ptr()
+        return fma_cache_batch_t(kp.data_ptr(), vp.data_ptr(), at_sum, npage, nsum, table.data_ptr(), at_stable, width,
+                                 cu.data_ptr(), start.data_ptr(), S, chunk, rows)
 
-    def _rows(self, t, name, heads, rows, dev):
-        """fma_view_t of [tokens, heads, d]."""
-        if t.shape != (rows, heads, self.head_dim):
-            _refuse(FMA_ERR_SHAPE, "%s has shape %s, expected %s", name, tuple(t.shape), (rows, heads, self.head_dim))
-        if t.dtype != self.dtype or t.device != dev:
-            _refuse(FMA_ERR_ARG, "%s is %s on %s, expected %s on %s", name, t.dtype, t.device, self.dtype, dev)
+    def _rows(self, t, name, heads, rows, gpu):
+        """The fields of the fma_view_t of [tokens, heads, d]."""
+        shape = (rows, heads, self.head_dim)
+        if t.shape != shape or t.dtype is not self.dtype or t.get_device() != gpu:
+            _explain(t, name, shape, self.dtype, gpu)
         s = t.stride()
         if s[2] != 1:
             _refuse(FMA_ERR_SHAPE, "the channels of %s are not adjacent", name)
-        return fma_view_t(t.data_ptr(), 0, s[1], s[0])
+        return t.data_ptr(), 0, s[1], s[0]
 
-    def _weights(self, wk, wv, dev):
+    def _weights(self, wk, wv, gpu):
         if not self.sets:
             return None, None
+        if wk is None or wv is None:
+            _refuse(FMA_ERR_NULL, "the plan's coarse sets need wk and wv")
         shape = (self.kv_heads, self.weights_len) if self.weights_per_head else (self.weights_len,)
-        for name, w in (("wk", wk), ("wv", wv)):
-            if w is None:
-                _refuse(FMA_ERR_NULL, "%s is None", name)
-            _plain(w, name, shape, torch.float32, dev)
+        _plain(wk, "wk", shape, torch.float32, gpu)
+        _plain(wv, "wv", shape, torch.float32, gpu)
         return wk, wv
 
     # ---------------------------------------------------------- calls
     def append(self, k, v, wk, wv, pages, batch, stream=None):
         """New keys and values [tokens, kv_heads, d] (any strides, adjacent
         channels) into the pages, and the summaries that they complete."""
-        rows, dev = k.shape[0], k.device
-        with _Launch(dev, stream):
-            wk, wv = self._weights(wk, wv, dev)
-            fma_cache_append(self.handle, self._batch(pages, batch, rows, dev),
-                             self._rows(k, "k", self.kv_heads, rows, dev), self._rows(v, "v", self.kv_heads, rows, dev),
-                             wk, wv)
+        rows, gpu, kv = k.shape[0], k.get_device(), self.kv_heads
+        with _launch(k, stream):
+            wk, wv = self._weights(wk, wv, gpu)
+            buf = _VIEWS[2](*self._rows(k, "k", kv, rows, gpu), *self._rows(v, "v", kv, rows, gpu))
+            at = ctypes.addressof(buf)
+            fma_cache_append(self.handle, self._batch(pages, batch, rows, gpu), at, at + _VIEW, wk, wv)
 
     def attend(self, q, pages, batch, out=None, stream=None):
         """Attention of q [tokens, heads, d], whose keys and values are in the
         cache, -> out (a new one is zero in rows of no sequence)."""
-        rows, dev = q.shape[0], q.device
-        with _Launch(dev, stream):
+        rows, gpu, h = q.shape[0], q.get_device(), self.heads
+        with _launch(q, stream):
             if out is None:
-                out = torch.zeros((rows, self.heads, self.head_dim), dtype=self.dtype, device=dev)
-            fma_cache_attend(self.handle, self._batch(pages, batch, rows, dev),
-                             self._rows(q, "q", self.heads, rows, dev), self._rows(out, "out", self.heads, rows, dev))
+                out = torch.zeros((rows, h, self.head_dim), dtype=self.dtype, device=q.device)
+            buf = _VIEWS[2](*self._rows(q, "q", h, rows, gpu), *self._rows(out, "out", h, rows, gpu))
+            at = ctypes.addressof(buf)
+            fma_cache_attend(self.handle, self._batch(pages, batch, rows, gpu), at, at + _VIEW)
         return out
 
     def step(self, q, k, v, wk, wv, pages, batch, out=None, stream=None):
         """append, then attend."""
-        rows, dev = q.shape[0], q.device
-        with _Launch(dev, stream):
-            wk, wv = self._weights(wk, wv, dev)
+        rows, gpu, h, kv = q.shape[0], q.get_device(), self.heads, self.kv_heads
+        with _launch(q, stream):
+            wk, wv = self._weights(wk, wv, gpu)
             if out is None:
-                out = torch.zeros((rows, self.heads, self.head_dim), dtype=self.dtype, device=dev)
-            fma_cache_step(self.handle, self._batch(pages, batch, rows, dev),
-                           self._rows(q, "q", self.heads, rows, dev), self._rows(k, "k", self.kv_heads, rows, dev),
-                           self._rows(v, "v", self.kv_heads, rows, dev), wk, wv,
-                           self._rows(out, "out", self.heads, rows, dev))
+                out = torch.zeros((rows, h, self.head_dim), dtype=self.dtype, device=q.device)
+            buf = _VIEWS[4](*self._rows(q, "q", h, rows, gpu), *self._rows(k, "k", kv, rows, gpu),
+                            *self._rows(v, "v", kv, rows, gpu), *self._rows(out, "out", h, rows, gpu))
+            at = ctypes.addressof(buf)
+            fma_cache_step(self.handle, self._batch(pages, batch, rows, gpu), at, at + _VIEW, at + 2 * _VIEW, wk, wv,
+                           at + 3 * _VIEW)
         return out

@@ -16,6 +16,8 @@
 // What bounds it: bytes; nothing is read twice.
 #include "qk_norm_rope.hpp"
 
+#include <type_traits>
+
 #include "row_lanes.hpp"
 
 namespace fma_dev {
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void qk_forward_kernel(QkArgs a, int per)
 
 // Backward.  Workgroup w walks token tiles w, w + groups, .. with all heads; its
 // sums of the gammas' gradients go to part[w].
-template <bool BF16, int D, bool IL>
+template <bool BF16, int D, bool IL, bool SHARED>
 __global__ __launch_bounds__(kThreads) void qk_backward_kernel(QkArgs a, int tiles, int ny, int per)
 {
     constexpr int LPR = D / 8, TPB = kThreads / LPR;
@@ -192,26 +194,21 @@ __global__ __launch_bounds__(kThreads) void qk_backward_kernel(QkArgs a, int til
         const bool live = row < a.rows;   // the others repeat row 0 and add and store nothing
         const int b = live ? (int)row / a.tokens : 0, t = live ? (int)row - b * a.tokens : 0;
         const Turn tu = token_turn<D, IL>(a, live ? row : 0, t, lane);
-        for (int i = lo; i < hi; ++i) {
-            const bool isq = i < a.heads, isv = i >= nqk;
-            const int h = isq ? i : isv ? i - nqk : i - a.heads;
-            const QkView &gv = isq ? a.qo : isv ? a.vo : a.ko;
-            const QkView &dv = isq ? a.dq : isv ? a.dv : a.dk;
-            const int rep = isq ? 1 : a.rep;
-            float g[8], x[8];
-            if (!isv) {
-                const QkView &xv = isq ? a.q : a.k;
-                floats<BF16>(load8<BF16>(xv, at(xv, b, h, t) + ch), x);
-            }
-            floats<BF16>(load8<BF16>(gv, at(gv, b, h * rep, t) + ch), g);
-            for (int m = 1; m < rep; ++m) {   // a shared head's gradients
-                float more[8];
-                floats<BF16>(load8<BF16>(gv, at(gv, b, h * rep + m, t) + ch), more);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] += more[j];
-            }
-            if (!isv) {
-                float z[8], ss = 0.f, ux = 0.f;
+        auto head = [&](int i) { return i < a.heads ? i : i < nqk ? i - a.heads : i - nqk; };
+        auto input = [&](int i) {   // (values have none: their gradient goes through)
+            const QkView &xv = i < a.heads ? a.q : a.k;
+            return i < nqk ? load8<BF16>(xv, at(xv, b, head(i), t) + ch) : Raw8<BF16>();
+        };
+        auto upstream = [&](int i, int m) {   // of copy m of the head
+            const QkView &gv = i < a.heads ? a.qo : i < nqk ? a.ko : a.vo;
+            return load8<BF16>(gv, at(gv, b, head(i) * (i < a.heads ? 1 : a.rep) + m, t) + ch);
+        };
+        // one row: its gradient g in, the input's out
+        auto finish = [&](int i, const Raw8<BF16> &raw, float (&g)[8]) __attribute__((always_inline)) {
+            const bool isq = i < a.heads;
+            if (i < nqk) {
+                float x[8], z[8], ss = 0.f, ux = 0.f;
+                floats<BF16>(raw, x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float other = IL ? g[j ^ 1] : __shfl(g[j], tu.peer);
@@ -236,7 +233,48 @@ __global__ __launch_bounds__(kThreads) void qk_backward_kernel(QkArgs a, int til
 #pragma unroll
                 for (int j = 0; j < 8; ++j) g[j] = rs * fmaf(-x[j], m, u[j]);
             }
-            if (live) store8<BF16>(dv, at(dv, b, h, t) + ch, rounded<BF16>(g));
+            const QkView &dv = isq ? a.dq : i < nqk ? a.dk : a.dv;
+            if (live) store8<BF16>(dv, at(dv, b, head(i), t) + ch, rounded<BF16>(g));
+        };
+        // heads of their own, two at a time: 4 KB per wave on the way
+        const int one = SHARED && hi > a.heads ? (lo > a.heads ? lo : a.heads) : hi;
+        for (int i0 = lo; i0 < one; i0 += 2) {
+            Raw8<BF16> x[2], g[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = i0 + u < one ? i0 + u : i0;
+                x[u] = input(i);
+                g[u] = upstream(i, 0);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (i0 + u >= one) continue;
+                float f[8];
+                floats<BF16>(g[u], f);
+                finish(i0 + u, x[u], f);
+            }
+        }
+        if constexpr (SHARED) {   // shared heads: their copies' gradients, four at a time
+            for (int i = one; i < hi; ++i) {
+                const Raw8<BF16> x = input(i);
+                float g[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) g[j] = 0.f;
+                for (int m0 = 0; m0 < a.rep; m0 += 4) {
+                    Raw8<BF16> more[4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) more[m] = upstream(i, m0 + m < a.rep ? m0 + m : m0);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        if (m0 + m >= a.rep) continue;
+                        float f[8];
+                        floats<BF16>(more[m], f);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) g[j] += f[j];
+                    }
+                }
+                finish(i, x, g);
+            }
         }
     }
     // the lanes of a channel across the wave, then the four waves
@@ -270,6 +308,7 @@ __global__ __launch_bounds__(1024) void qk_gamma_kernel(QkArgs a, int groups)
 {
     const int col = 16 * blockIdx.x + (threadIdx.x & 15), d = a.head_dim;
     float s = 0.f;
+#pragma unroll 8
     for (int g = threadIdx.x >> 4; g < groups; g += 64) s += a.part[(long long)g * 2 * d + col];
     __shared__ float part[64][17];
     part[threadIdx.x >> 4][threadIdx.x & 15] = s;
@@ -291,7 +330,7 @@ int tasks_per_group(long long tiles, int tasks, long long want)
     return (int)((tasks + split - 1) / split);
 }
 
-constexpr long long kForwardGroups = 1024, kBackwardGroups = 2048;
+constexpr long long kForwardGroups = 1024, kBackwardGroups = 1024;
 
 long long token_tiles(long long rows, int d) { return (rows + kThreads / (d / 8) - 1) / (kThreads / (d / 8)); }
 
@@ -334,14 +373,14 @@ hipError_t backward_d(const QkArgs &a, hipStream_t st)
     BackwardGrid g = {0, 0, 0};   // no rows: the gammas' gradients are sums of nothing
     if (a.rows) g = backward_grid(a.rows, tasks, D);
     const int tiles = (int)token_tiles(a.rows, D);
-    if (g.groups == 0)
-        ;
-    else if (a.interleaved)
-        hipLaunchKernelGGL((qk_backward_kernel<BF16, D, true>), dim3((unsigned)g.groups), dim3(kThreads), 0, st, a,
-                           tiles, g.ny, g.per);
-    else
-        hipLaunchKernelGGL((qk_backward_kernel<BF16, D, false>), dim3((unsigned)g.groups), dim3(kThreads), 0, st, a,
-                           tiles, g.ny, g.per);
+    auto launch = [&](auto il, auto shared) {
+        hipLaunchKernelGGL((qk_backward_kernel<BF16, D, decltype(il)::value, decltype(shared)::value>), dim3((unsigned)g.groups),
+                           dim3(kThreads), 0, st, a, tiles, g.ny, g.per);
+    };
+    typedef std::true_type Yes;
+    typedef std::false_type No;
+    if (g.groups && a.interleaved) a.rep > 1 ? launch(Yes(), Yes()) : launch(Yes(), No());
+    if (g.groups && !a.interleaved) a.rep > 1 ? launch(No(), Yes()) : launch(No(), No());
     if (a.dgamma_q || a.dgamma_k)
         hipLaunchKernelGGL(qk_gamma_kernel, dim3(2 * D / 16), dim3(1024), 0, st, a, (int)g.groups);
     return hipGetLastError();

@@ -126,7 +126,7 @@ def test_batch_refusals(plan, change, status):
 def test_call_refusals(plan):
     b, x = _batch(), _views()
     assert _calls(None, b, x) == [F.FMA_ERR_NULL] * 3
-    assert F.library().fma_cache_append(plan, None, x["k"], x["v"], None, None, None) == F.FMA_ERR_NULL
+    assert F.library().fma_cache_append(plan, None, F._ref(x["k"]), F._ref(x["v"]), None, None, None) == F.FMA_ERR_NULL
     step = lambda **kw: _status(F.fma_cache_step, plan, b, *[kw.get(n, x.get(n)) for n in ("q", "k", "v")],  # noqa: E731
                                 kw.get("wk", MB * 90), kw.get("wv", MB * 91), kw.get("out", x["out"]), 0)
     for n in ("q", "k", "v", "out"):
@@ -159,8 +159,8 @@ def test_calls_without_tokens_need_nothing(plan, change):
 
 def test_object_refusals():
     op = F.FMACache(4, 4096, kv_heads=2)
-    cpu = torch.device("cpu")
-    pages = op.new_pages(3, 3, cpu)
+    cpu = -1      # (the device number of CPU tensors)
+    pages = op.new_pages(3, 3, "cpu")
     z = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
     b = F.CacheBatch(z(3), z(2), z(2, 5), z(2, 5), 4)
     k = torch.zeros(7, 2, 64, dtype=torch.bfloat16)

@@ -191,11 +191,8 @@ def test_object_refusals():
     with pytest.raises(F.FmaError) as e:
         op.forward(x[0], x[:, :, :2])
     assert e.value.status == F.FMA_ERR_SHAPE
-    with pytest.raises(F.FmaError):
-        F._view(x, "q", (1, 3, 2, 64), F._TOKEN_MAJOR, torch.bfloat16, x.device)
-    with pytest.raises(F.FmaError):
-        F._view(x, "q", (1, 3, 4, 64), F._TOKEN_MAJOR, torch.float32, x.device)
-    with pytest.raises(F.FmaError):
-        F._view(x.expand(1, 3, 4, 64).transpose(2, 3), "q", (1, 3, 64, 4), F._TOKEN_MAJOR, torch.bfloat16, x.device)
-    v = F._view(x, "q", (1, 3, 4, 64), F._TOKEN_MAJOR, torch.bfloat16, x.device)
-    assert (v.batch_stride, v.head_stride, v.token_stride) == (768, 64, 256)
+    view = lambda t, shape, dtype=torch.bfloat16: F._view(t, "q", shape, F._TOKEN_MAJOR, dtype, -1)  # noqa: E731
+    assert _status(view, x, (1, 3, 2, 64)) == F.FMA_ERR_SHAPE
+    assert _status(view, x, (1, 3, 4, 64), torch.float32) == F.FMA_ERR_ARG
+    assert _status(view, x.transpose(2, 3), (1, 3, 64, 4)) == F.FMA_ERR_SHAPE
+    assert view(x, (1, 3, 4, 64)) == (x.data_ptr(), 768, 64, 256)
