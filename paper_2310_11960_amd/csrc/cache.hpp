@@ -139,7 +139,7 @@ inline bool cache_launches_fit(const CacheArgs &a, bool appends, bool attends, i
 
 hipError_t launch_cache_append(const CacheArgs &a, hipStream_t st);
 hipError_t launch_cache_token(const CacheArgs &a, hipStream_t st);
-hipError_t launch_cache_keys(const CacheArgs &a, const ChunkShape &c, hipStream_t st);
+hipError_t launch_cache_keys(const CacheArgs &a, const ChunkShape &c, int cus, hipStream_t st);
 hipError_t launch_cache_rows(const CacheArgs &a, const ChunkShape &c, hipStream_t st);
 
 // A workgroup's tile: positions [pos, pos + n) of sequence seq, the first in row

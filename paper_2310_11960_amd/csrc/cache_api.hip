@@ -40,11 +40,11 @@ struct Call {
 };
 
 // The attention of a call (a.write: with the new tokens' way into the cache).
-hipError_t launch_attention(const CacheArgs &a, CacheRoute route, hipStream_t st)
+hipError_t launch_attention(const CacheArgs &a, CacheRoute route, int cus, hipStream_t st)
 {
     if (route == CACHE_TOKENS) return launch_cache_token(a, st);
     const ChunkShape c = chunk_shape(a);
-    return route == CACHE_KEYS ? launch_cache_keys(a, c, st) : launch_cache_rows(a, c, st);
+    return route == CACHE_KEYS ? launch_cache_keys(a, c, cus, st) : launch_cache_rows(a, c, st);
 }
 
 // Checks everything of a call; *skip: no rows, nothing to do.
@@ -214,7 +214,8 @@ fma_status_t fma_cache_attend(fma_cache_plan_t plan, const fma_cache_batch_t *ba
     const fma_status_t st = check_call(c, a, &skip);
     if (st) return st;
     if (skip) return set_status(FMA_OK, nullptr);
-    return status_of(c.fn, launch_attention(a, cache_route(a, compute_units()), static_cast<hipStream_t>(stream)));
+    const int cus = compute_units();
+    return status_of(c.fn, launch_attention(a, cache_route(a, cus), cus, static_cast<hipStream_t>(stream)));
 }
 
 fma_status_t fma_cache_step(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
@@ -230,11 +231,12 @@ fma_status_t fma_cache_step(fma_cache_plan_t plan, const fma_cache_batch_t *batc
     if (st) return st;
     if (skip) return set_status(FMA_OK, nullptr);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const CacheRoute route = cache_route(a, compute_units());
+    const int cus = compute_units();
+    const CacheRoute route = cache_route(a, cus);
     a.write = route != CACHE_ROWS && a.max_chunk <= a.r;
     hipError_t e = hipSuccess;
     if (!a.write) e = launch_cache_append(a, s);
-    if (e == hipSuccess) e = launch_attention(a, route, s);
+    if (e == hipSuccess) e = launch_attention(a, route, cus, s);
     return status_of(c.fn, e);
 }
 

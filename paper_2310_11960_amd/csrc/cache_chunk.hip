@@ -5,34 +5,20 @@
 // one key head) and meet every 32-row tile of keys in LDS: the previous and the
 // own block's tokens, which stream through two stages by direct-to-LDS loads
 // a tile ahead, then the far list, loaded once at the start.  A wave leaves
-// out the tiles behind its last query.  Per tile:
-//   S^T = K Q^T (row reads), P = exp2(c s - m), l += the sum of P,
-//   O^T += V^T P^T (bf16: transposing reads)
-// on v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32.  m follows a query's
-// maximum when that passes it by 2^8: a smaller lead only scales P, which rounds
-// to bf16 alike at any scale, and l adds the rounded P, so that a dominating
-// source still weighs exactly 1.
+// out the tiles behind its last query.  Products and softmax: cache_tile.hpp.
 //
 // What bounds it: issue.  A 32 x 32 piece at d = 64 takes 256 cycles of matrix
 // products and about 450 of vector work, the exponentials 256 of them; row
 // addresses per lane and a maximum per tile made it 1500 (26 us a workgroup).
 #include "cache_device.hpp"
+#include "cache_tile.hpp"
 #include "row_groups.hpp"
-#include "wave_ops.hpp"
 
 namespace fma_dev {
 
 namespace {
 
 constexpr int kStages = 2;   // near tiles in LDS
-
-// A row's 16-byte chunk c lies at chunk c ^ chunk_swz(row).
-template <bool BF16, int D>
-__device__ inline int chunk_swz(int row)
-{
-    if constexpr (BF16) return swzd<D>(row);
-    else return row & (D == 32 ? 7 : 15);
-}
 
 // Rows of a block's tokens: position p of [lo, hi) at k + (p - first) * sk, v likewise.
 template <bool BF16>
@@ -65,10 +51,10 @@ struct NearRows {
 };
 
 template <bool BF16, int D, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 ? 1 : D == 128 ? 2 : 4)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW < 4 ? 1 : BF16 ? (D == 128 ? 2 : 4) : (D == 32 ? 4 : 1))))
 void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs, int far_cap)
 {
-    constexpr int ND = D / 32, NC = BF16 ? D / 16 : D / 8, RB = D * (BF16 ? 2 : 4), TB = 32 * RB;   // row, tile bytes
+    constexpr int ND = D / 32, RB = D * (BF16 ? 2 : 4), TB = 32 * RB;   // row, tile bytes
     constexpr int CPR = RB / 16, RPL = 64 / CPR, NLD = TB / 1024;   // 16-byte chunks of a row, rows of a load, loads
     constexpr int ML = (2 * NLD + NW - 1) / NW, FL = 2 * NLD / NW;  // a wave's loads of a tile, at most and at least
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -171,40 +157,21 @@ void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs, int far_cap)
     for (int i = 0; i < kStages - 1; ++i)
         if (i < near) issue(i, i);
 
-    // this lane's query; a negative scale turns its sign, so that the greatest
-    // product is the greatest score
+    // this lane's query
     const int rows = x.n * ng, row = 32 * wave + l32, qi = row < rows ? row / ng : 0, gi = row < rows ? row - qi * ng : 0;
     const int qpos = x.pos + qi;
     const int wfirst = x.pos + 32 * wave / ng;   // positions of the wave's first and last rows
     const int wtop = 32 * wave + 31 < rows ? 32 * wave + 31 : rows - 1, wlast = x.pos + wtop / ng;
     const bool active = 32 * wave < rows;
-    const float scale = fabsf(a.scale_log2);
-    uint4 qo[NC];
-    {
-        const char *p = static_cast<const char *>(elem<BF16>(a.q, (long long)(x.row + qi) * a.qt + (h * a.group + g0 + gi) * a.qh)) + 16 * hh;
-        const uint32_t sign = a.scale_log2 < 0.f ? (BF16 ? 0x80008000u : 0x80000000u) : 0u;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            qo[c] = *reinterpret_cast<const uint4 *>(p + 32 * c);
-            qo[c].x ^= sign, qo[c].y ^= sign, qo[c].z ^= sign, qo[c].w ^= sign;
-        }
-    }
+    QueryTile<BF16, D> qt(lane, a.scale_log2);
+    qt.load(elem<BF16>(a.q, (long long)(x.row + qi) * a.qt + (h * a.group + g0 + gi) * a.qh), a.scale_log2);
     if (list.n) far_rows(0);
-
+    qt.start(lane);
     f32x16 o[ND];
 #pragma unroll
     for (int db = 0; db < ND; ++db) o[db] = f32x16{0};
     float m = -INFINITY, l = 0.f;
-    const int koff = l32 * RB + 16 * (hh ^ chunk_swz<BF16, D>(l32));
-    int voff[2];
-    {
-        const int gq = lane >> 4, s4 = lane & 15, jr = s4 >> 2, qq = s4 & 3;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int r = 8 * k + 4 * (gq >> 1) + jr;
-            voff[k] = r * D + 8 * ((2 * (gq & 1) + (qq >> 1)) ^ swzd<D>(r)) + 4 * (qq & 1);
-        }
-    }
+
     const int tiles = near + (list.n + 31) / 32;
 #pragma unroll 1
     for (int i = 0; i < tiles; ++i) {
@@ -241,76 +208,7 @@ void cache_chunk_kernel(CacheArgs a, Tiling t, int split, int gs, int far_cap)
             last = 31;
             all = vm == ~0u;
         }
-        f32x16 s = {0};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            if constexpr (BF16) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + (koff ^ (32 * c)));
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, qo[c]), s, 0, 0, 0);
-            } else {
-                const f32x4 kf = *reinterpret_cast<const f32x4 *>(kt + (koff ^ (32 * c)));
-                const f32x4 qf = __builtin_bit_cast(f32x4, qo[c]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j], qf[j], s, 0, 0, 0);
-            }
-        }
-        if (!all) {
-            const uint32_t see = seen_rows(vm, last, hh);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[j] = seen(see, j) ? s[j] : -INFINITY;
-        }
-        float mx = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) mx = __builtin_elementwise_maximum(mx, s[j]);
-        mx = pair_max(mx) * scale;
-        const bool up = mx > m + 8.f || m == -INFINITY;
-        if (__builtin_amdgcn_ballot_w64(up) != 0) {
-            const float mnew = up ? mx : m;
-            const float corr = mnew == m ? 1.f : __builtin_amdgcn_exp2f(m - mnew);   // (-inf: still nothing seen)
-            m = mnew;
-            l *= corr;
-#pragma unroll
-            for (int db = 0; db < ND; ++db)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[db][j] *= corr;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale, -ref));
-        if constexpr (BF16) {
-            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-            const bf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    w[k] = pack_bf16(s[8 * hf + 2 * k], s[8 * hf + 2 * k + 1]);
-                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[k]), ones, l, false);
-                }
-                const uint4 pw = make_uint4(w[0], w[1], w[2], w[3]);
-                const __bf16 *const v16 = reinterpret_cast<const __bf16 *>(vt) + 16 * hf * D;
-#pragma unroll
-                for (int db = 0; db < ND; ++db) {
-                    const s16x4 r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v16 + (voff[0] ^ (32 * db))));
-                    const s16x4 r2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v16 + (voff[1] ^ (32 * db))));
-                    const s16x8 av = {r1[0], r1[1], r1[2], r1[3], r2[0], r2[1], r2[2], r2[3]};
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av),
-                                                                    __builtin_bit_cast(bf16x8, pw), o[db], 0, 0, 0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                l += s[j];
-                const int r = grow(j, hh), sw = chunk_swz<BF16, D>(r);
-#pragma unroll
-                for (int db = 0; db < ND; ++db) {
-                    const float vf = *reinterpret_cast<const float *>(vt + r * RB + 16 * ((8 * db + (l32 >> 2)) ^ sw) + 4 * (l32 & 3));
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[j], o[db], 0, 0, 0);
-                }
-            }
-        }
+        qt.meet(kt, vt, seen_rows(vm, last, hh), all, o, m, l);
     }
     if (!active) return;
     l = pair_sum(l);
