@@ -2,10 +2,11 @@
 // the matrix cores:
 //   S^T = K Q^T (row reads), P = exp2(c s - m), l += the sum of P,
 //   O^T += V^T P^T (bf16: transposing reads)
-// on v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32.  m follows a query's
-// maximum when that passes it by 2^8: a smaller lead only scales P, which rounds
-// to bf16 alike at any scale, and l adds the rounded P, so that a dominating
-// source still weighs exactly 1.
+// on v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32.  m is the running maximum
+// and l adds P as bf16 has rounded it, so that a dominating source weighs exactly
+// 1.  (A reference that follows only when passed by 2^8 was 4 % faster at d = 64
+// and its error against float64 up to 6 % larger.)  m, l and O are fp32; P is
+// rounded to bf16 for the second product, V's type.
 #pragma once
 
 #include "lds_rows.hpp"
@@ -104,7 +105,7 @@ struct QueryTile {
 #pragma unroll
         for (int j = 1; j < 16; ++j) mx = __builtin_elementwise_maximum(mx, s[j]);
         mx = pair_max(mx) * scale;
-        const bool up = mx > m + 8.f || m == -INFINITY;
+        const bool up = mx > m || m == -INFINITY;
         if (__builtin_amdgcn_ballot_w64(up) != 0) {
             const float mnew = up ? mx : m;
             const float corr = mnew == m ? 1.f : __builtin_amdgcn_exp2f(m - mnew);   // (-inf: still nothing seen)
