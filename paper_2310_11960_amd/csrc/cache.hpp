@@ -37,20 +37,22 @@ struct Tiling {
 
 __host__ __device__ inline int tile_of(const Tiling &t, int r, int pos) { return pos / r * t.tpb + pos % r / t.tm; }
 
-// Tiles of tm positions over chunks of at most a.max_chunk tokens.  A window of w
-// positions holds at most w tpb / r + 2 tile starts, so the rows tpb / r + 3 S
-// tiles bound any batch, and a tile has at least one row.  One tile range per
-// sequence, without a search, where that leaves at most twice as many idle
-// workgroups.
+// Tiles of tm positions over chunks of at most a.max_chunk tokens.  A chunk of w
+// tokens meets 1 + ceil((w - 1) / tm) tiles at most where tiles of tm fill a
+// block; where a block ends with a shorter one, no more than w tpb / r + 3; so
+// rows / tm + 2 S (rows tpb / r + 3 S) bound any batch, and a tile has at least one
+// row.  One tile range per sequence, without a search, where that leaves at most
+// twice as many idle workgroups.
 inline Tiling make_tiling(const CacheArgs &a, int tm)
 {
     Tiling t;
     t.tm = tm < a.r ? tm : a.r;
     t.tpb = (a.r + t.tm - 1) / t.tm;
+    const bool even = t.tpb * t.tm == a.r;
     const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
-    long long each = most * t.tpb / a.r + 3;
+    long long each = even ? (most + t.tm - 2) / t.tm + 1 : most * t.tpb / a.r + 3;
     if (each > most) each = most;
-    long long bound = (long long)a.rows * t.tpb / a.r + 3LL * a.S;
+    long long bound = even ? a.rows / t.tm + 2LL * a.S : (long long)a.rows * t.tpb / a.r + 3LL * a.S;
     if (bound > a.rows) bound = a.rows;
     t.per_seq = each * a.S <= 2 * bound + 64 ? (int)each : 0;
     t.units = t.per_seq ? each * a.S : bound;
