@@ -140,6 +140,7 @@ __global__ __launch_bounds__(64 * NW) void cache_keys_kernel(CacheArgs a, Tiling
 #pragma unroll
     for (int db = 0; db < ND; ++db) o[db] = f32x16{0};
     float m = -INFINITY, l = 0.f;
+    uint32_t late = 0;   // near tiles (16 at most) that come at the end
     char *const tile = sm.tile[wave];
 #pragma unroll 1
     for (int i = wave; i < tiles; i += NW) {
@@ -152,8 +153,14 @@ __global__ __launch_bounds__(64 * NW) void cache_keys_kernel(CacheArgs a, Tiling
         put(tile, rv);
         const int last = i < near ? qpos - klo - 32 * i : 31;
         const bool all = vm == ~0u && (i >= near || klo + 32 * i + 31 <= x.pos);
+        if (!all && i < near && qt.odd_rows(tile)) {
+            late |= 1u << i;
+            continue;
+        }
         qt.meet(kf, tile, seen_rows(vm, last, hh), all, o, m, l);
     }
+    for (; late; late &= late - 1)
+        late_rows<BF16, D>(a, x, h, klo + 32 * __builtin_ctz(late), qt, qpos, o, m, l);
 
     // the waves' parts: a common reference, then 32 channels at a time
     l = pair_sum(l);

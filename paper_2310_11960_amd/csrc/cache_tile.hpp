@@ -7,9 +7,15 @@
 // 1.  (A reference that follows only when passed by 2^8 was 4 % faster at d = 64
 // and its error against float64 up to 6 % larger.)  m, l and O are fp32; P is
 // rounded to bf16 for the second product, V's type.
+//
+// A weight of 0 does not hide an infinity or a NaN in a matrix product.  Where
+// queries may lie before rows of a tile and a value row holds one (odd_rows), the
+// kernel leaves the tile out and takes its rows one by one at the end, each for
+// the queries that see it (late_rows).  This costs a few registers and a look at
+// one or two tiles of a wave: 12 long pieces at rank 4 88.6 -> 93.2 us.
 #pragma once
 
-#include "lds_rows.hpp"
+#include "cache_device.hpp"
 #include "wave_ops.hpp"
 
 namespace fma_dev {
@@ -60,8 +66,29 @@ struct QueryTile {
             qo[c].x ^= sign, qo[c].y ^= sign, qo[c].z ^= sign, qo[c].w ^= sign;
         }
     }
+    // whether value rows of a tile hold an infinity or a NaN
+    __device__ __attribute__((always_inline)) bool odd_rows(const char *vt) const
+    {
+        float z[4] = {0.f, 0.f, 0.f, 0.f};   // x * 0 is 0 but for those
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(vt + (koff ^ (32 * c)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (BF16) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    const bf16x2 none = {static_cast<__bf16>(0.f), static_cast<__bf16>(0.f)};
+                    const float w = x[j];
+                    z[j] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), none, z[j], false);
+                } else {
+                    z[j] = fmaf(x[j], 0.f, z[j]);
+                }
+            }
+        }
+        return __builtin_amdgcn_ballot_w64((z[0] + z[1]) + (z[2] + z[3]) != 0.f) != 0;
+    }
     // rows kt, vt (RB bytes each, swizzled); see: seen_rows of this lane's query; all: every
-    // query of the wave sees every row.  o: O^T, channels 32 db + grow(j, lane >> 5);
+    // query of the wave sees every row; odd: value rows to leave out.  o: O^T, channels 32 db + grow(j, lane >> 5);
     // m, l: reference and this lane's part of the sum, log2 units.  (They are the
     // kernel's own variables: as members they cost a second copy of o.)
     __device__ __attribute__((always_inline)) void meet(const char *kt, const char *vt, uint32_t see, bool all,
@@ -155,6 +182,63 @@ struct QueryTile {
         }
     }
 };
+
+// The near rows of positions k0 .. k0 + 31, one by one, for the queries (at qpos)
+// that see them.
+template <bool BF16, int D>
+__device__ inline void late_rows(const CacheArgs &a, const Tile &x, int h, int k0, const QueryTile<BF16, D> &qt, int qpos,
+                                 f32x16 (&o)[D / 32], float &m, float &l)
+{
+    const int end = k0 + 32 < x.pos + x.n ? k0 + 32 : x.pos + x.n;
+    for (int pos = k0; pos < end; ++pos) {
+        const char *k, *v;
+        const int page = page_of(a, x.seq, pos / a.r);
+        if (a.k && pos >= x.start) {
+            const long long n = x.row0 + pos - x.start;
+            k = static_cast<const char *>(elem<BF16>(a.k, n * a.kt + h * a.kh));
+            v = static_cast<const char *>(elem<BF16>(a.v, n * a.vt + h * a.vh));
+        } else if (page >= 0) {
+            const long long off = page_row(a, page, h, pos % a.r);
+            k = static_cast<const char *>(elem<BF16>(const_cast<const void *>(a.kp), off));
+            v = static_cast<const char *>(elem<BF16>(const_cast<const void *>(a.vp), off));
+        } else {
+            continue;
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < qt.NC; ++c) {
+            constexpr int W = BF16 ? 8 : 4;   // channels of a 16-byte chunk
+            const uint4 w = qt.qo[c];
+            const uint32_t qw[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const int ch = (2 * c + qt.hh) * W + j;
+                if constexpr (BF16)
+                    s = fmaf(__uint_as_float(j & 1 ? qw[j / 2] & 0xffff0000u : qw[j / 2] << 16),
+                             static_cast<float>(reinterpret_cast<const __bf16 *>(k)[ch]), s);
+                else
+                    s = fmaf(__uint_as_float(qw[j]), reinterpret_cast<const float *>(k)[ch], s);
+            }
+        }
+        s = pair_sum(s) * qt.scale;
+        if (pos > qpos) continue;
+        const float top = fmaxf(m, s), ref = top == -INFINITY ? 0.f : top;
+        const float corr = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(s - ref);
+        m = top;
+        l = l * corr + (qt.hh ? 0.f : p);   // (a lane's part)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int ch = 32 * db + grow(j, qt.hh);
+                float y;
+                if constexpr (BF16) y = static_cast<float>(reinterpret_cast<const __bf16 *>(v)[ch]);
+                else y = reinterpret_cast<const float *>(v)[ch];
+                o[db][j] = fmaf(p, y, o[db][j] * corr);
+            }
+        }
+    }
+}
 
 }  // namespace
 

@@ -115,6 +115,7 @@ __global__ __launch_bounds__(kThreads) void cache_token_kernel(CacheArgs a, Tili
                 float f[8];
                 floats<BF16>(v[u], f);
                 l[i] += p;
+                if (R > 1 && s[u] == -INFINITY) continue;   // (0 times a later row's infinity is no number)
 #pragma unroll
                 for (int c = 0; c < 8; ++c) o[i][c] = fmaf(p, f[c], o[i][c]);
             }

@@ -306,6 +306,46 @@ def test_missing_pages_hide_their_tokens(dtype):
     assert ((out[0] - one).abs() <= 2 * R.HALF[DT[dtype]] * one.abs()).all()      # the first sees itself alone
 
 
+ODD = [(2, 2, 64, 64, [100, 3], [4, 3]), (4, 2, 32, 16, [20, 40], [13, 16]), (4, 2, 64, 64, [70, 0], [5, 60]),
+       (8, 2, 128, 64, [64, 130], [40, 62]), (16, 16, 64, 64, [30, 64] * 4, [300, 128] * 4),
+       (16, 16, 32, 16, [7, 64] * 4, [190, 128] * 4), (8, 4, 128, 128, [130, 64] * 4, [300, 128] * 4)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("shape", ODD, ids=lambda s: "-".join(map(str, s[:4] + (len(s[4]),))))
+@pytest.mark.parametrize("what", ["values", "keys"])
+def test_no_number_reaches_an_earlier_query(shape, dtype, what):
+    # an infinity and a NaN among a piece's own tokens: in a value's channel they stay in
+    # that channel of the queries from the token on; in a key, in those queries
+    heads, kv, d, r, before, take = shape
+    s = Served([a + b for a, b in zip(before, take)], heads, kv, d, r, max_len=1000, dtype=DT[dtype], seed=43)
+    s.step(before) if any(before) else None
+    at = [(n // 3, n - n // 4 - 1) for n in take]     # (row of the piece, its odd tokens)
+    q, k, v = (s.rows(x, take) for x in (s.q, s.k, s.v))
+    off = [sum(take[:i]) for i in range(len(take))]
+    for o, (j0, j1) in zip(off, at):
+        if what == "values":
+            v[o + j0, :, 5], v[o + j1, :, d - 3] = float("inf"), float("nan")
+        else:
+            k[o + j0, :, 5], k[o + j1, :, d - 3] = float("nan"), float("inf")
+    out = torch.full_like(q, 7.0)
+    s.op.step(q, k, v, *s.weights(), s.pages, s.batch(take), out=out)
+    out = out.cpu().double()
+    for i, (o, (j0, j1), n) in enumerate(zip(off, at, take)):
+        for h in range(0, heads, max(1, heads // 4)):
+            ref, bound = s.reference(i, h, before[i], before[i] + n)
+            got, good = out[o:o + n, h], torch.ones(n, d, dtype=torch.bool)
+            if what == "values":
+                good[j0:, 5] = False
+                good[j1:, d - 3] = False
+                assert not torch.isfinite(got[~good]).any(), (i, h)
+            else:
+                good[j0:] = False
+                assert torch.isnan(got[j0:]).all(), (i, h)
+            bad = ((got - ref).abs() > bound) | ~torch.isfinite(got)
+            assert not (bad & good).any(), (i, h, (bad & good).nonzero()[:4].tolist())
+
+
 def test_sequences_that_do_not_fit_are_skipped():
     r = 32
     s = Served([100, 100, 100, 100, 100, 100], 2, 2, 64, r, 1, max_len=128)
