@@ -60,13 +60,19 @@ inline Tiling make_tiling(const CacheArgs &a, int tm)
 }
 
 // Which kernel attends:
-//   TOKENS  at most four query rows meet a key head's rows, too few for a
-//           32-column matrix operand: the vector ALU (cache_token.hip);
+//   TOKENS  at most token_rows(a) query rows meet a key head's rows, too few for a
+//           32-column matrix operand: the vector ALU (cache_token.hip).  64
+//           sequences, TOKENS against KEYS: one row 20.8 against 40.8 us (fp32),
+//           two rows 16.1 against 19.9 (bf16, d = 64), four rows 20.4 against 23.6
+//           (d = 128) and 13.8 against 18.0 (fp32), but 14.8 against 12.3 (bf16,
+//           d = 64: the products of eight channels cost more than the loads);
 //   KEYS    32 rows a workgroup, whose waves take different keys
 //           (cache_attend.hip): pieces whose rows with one key head fit one
 //           such tile, and calls of too few rows to fill the device with
 //   ROWS    128 rows a workgroup, whose waves take different rows and share the
-//           keys in LDS (cache_chunk.hip).
+//           keys in LDS (cache_chunk.hip).  One piece, 16 heads, KEYS against
+//           ROWS: 1024 tokens (128 workgroups) 27.7 against 31.2 us, 2048 (256)
+//           39.9 against 33.5.
 // The first two put new tokens into the cache as well, where no chunk is longer
 // than a block (the far field of such a chunk has nothing of its own).
 enum CacheRoute { CACHE_TOKENS, CACHE_KEYS, CACHE_ROWS };
@@ -86,10 +92,12 @@ inline ChunkShape chunk_shape(const CacheArgs &a)
     return c;
 }
 
+inline int token_rows(const CacheArgs &a) { return a.bf16 && a.head_dim <= 64 ? 2 : 4; }
+
 inline CacheRoute cache_route(const CacheArgs &a, int cus)
 {
     const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
-    if (most * a.group <= 4) return CACHE_TOKENS;
+    if (most * a.group <= token_rows(a)) return CACHE_TOKENS;
     const ChunkShape c = chunk_shape(a);
     const long long groups = (long long)a.rows * c.gs / (c.tm * c.gs < 128 ? c.tm * c.gs : 128) * a.kv_heads * c.split;
     return most * c.gs <= 32 || groups < cus ? CACHE_KEYS : CACHE_ROWS;

@@ -257,7 +257,9 @@ hipError_t token_d(const CacheArgs &a, hipStream_t st)
     switch (token_tile(a) * a.group) {
     case 1: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 1>), grid, dim3(kThreads), 0, st, a, t); break;
     case 2: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 2>), grid, dim3(kThreads), 0, st, a, t); break;
-    default: hipLaunchKernelGGL((cache_token_kernel<BF16, D, 4>), grid, dim3(kThreads), 0, st, a, t); break;
+    default:   // (token_rows)
+        if constexpr (!BF16 || D > 64) hipLaunchKernelGGL((cache_token_kernel<BF16, D, 4>), grid, dim3(kThreads), 0, st, a, t);
+        else return hipErrorInvalidValue;
     }
     return hipGetLastError();
 }
