@@ -428,9 +428,10 @@ typedef struct fma_cache_plan_s *fma_cache_plan_t;   /* opaque, host-side, immut
  *     pages and summary pages, and a sequence can go back to any length whose
  *     pages it still has by naming that length;
  *   - the page of block b is no longer read once the sequence is past block
- *     b + 1; the summary page of block b is read while b is the block before
- *     the newest, and at level l (from 1) while b is the last block of one of
- *     the two groups before the newest query's parent pair of groups and after. */
+ *     b + 1.  For a newest token in block b, with q = b >> l at level l = 0, 1, ..,
+ *     the summary pages read are those of block b - 1 and of the last blocks
+ *     ((g + 1) << l) - 1 of the groups g = q - 2 and, for odd q, q - 3; a summary page
+ *     that is none of these for this and every later b can be given back. */
 typedef struct {
     int32_t struct_size;      /* sizeof(fma_cache_desc_t) */
     int32_t dtype;            /* fma_dtype_t */
@@ -484,8 +485,13 @@ typedef struct {
  *     skipped: nothing of it is read or written.  Rows of no sequence are
  *     left as they were.
  *   - A table entry outside the pool is a missing page: its tokens are neither
- *     written nor seen by queries of other calls, its sums count as zero.  A row that sees
- *     nothing is zero.
+ *     written nor seen by queries of other calls, its far rows are not seen, and
+ *     sums that would go on from it start from zero.  A row that sees nothing is
+ *     zero.
+ *   - A NaN or an infinity stays where the formulas put it: it reaches no query
+ *     before its token, and no other channel of the values.
+ *   - At most 2^21 rows and 2^20 sequences; fewer where rows x heads would not
+ *     fit one launch (FMA_ERR_SHAPE).
  *   - Pages written by a call must not be shared by its sequences.
  *   - Calls on one cache are ordered by the caller (one stream); they may be
  *     repeated with the same result, no atomics. */
@@ -501,8 +507,9 @@ fma_status_t fma_cache_append(fma_cache_plan_t plan, const fma_cache_batch_t *ba
 fma_status_t fma_cache_attend(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
                               const fma_view_t *out, void *stream);
 
-/* fma_cache_append, then fma_cache_attend, in one launch where no sequence has
- * more than `block` new tokens.  A row always sees its own token here. */
+/* fma_cache_append, then fma_cache_attend; in one launch where no sequence has
+ * more than `block` new tokens and the rows are too few to fill the device with
+ * tiles of 128.  A row always sees its own token here. */
 fma_status_t fma_cache_step(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
                             const fma_view_t *k, const fma_view_t *v, const float *wk, const float *wv,
                             const fma_view_t *out, void *stream);

@@ -472,6 +472,36 @@ def test_graph_replays_with_other_lengths():
             s.have = [h + t for h, t in zip(s.have, take)]
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+def test_graph_replays_of_longer_pieces(dtype):
+    r, H, rows, most = 64, 16, 2300, 1200
+    s = Served([r * 40, r * 40], H, H, 128, r, 2, dtype=DT[dtype], seed=44)
+    s.step([100, 700], "append")
+    w = s.weights()
+    buf = [torch.zeros(rows, H, 128, dtype=s.dtype, device=s.dev) for _ in range(3)]
+    out = torch.zeros_like(buf[0])
+    b = s.batch([0, 0], max_chunk=most)
+    s.op.step(*buf, *w, s.pages, b, out=out)   # warm, nothing new
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.op.step(*buf, *w, s.pages, b, out=out)
+    for take in ([1100, 1100], [1200, 1], [0, 600]):
+        for t, x in zip(buf, (s.q, s.k, s.v)):
+            new = s.rows(x, take)
+            t[:new.shape[0]] = new
+        for t, x in zip(b[:4], s.batch(take, max_chunk=most)[:4]):
+            t.copy_(x)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        s.check(got, take)
+        assert (got[sum(take):] == 7.0).all()
+        assert torch.equal(s.op.step(*buf, *w, s.pages, b)[:sum(take)], got[:sum(take)])
+        s.have = [h + t for h, t in zip(s.have, take)]
+    s.check_pages()
+
+
 def test_pools_past_32_bit_offsets():
     """Pages whose elements lie beyond 2^31 and 2^32 bytes."""
     dev = _dev()
