@@ -68,11 +68,18 @@ inline Tiling make_tiling(const CacheArgs &a, int tm)
 //           d = 64: the products of eight channels cost more than the loads);
 //   KEYS    32 rows a workgroup, whose waves take different keys
 //           (cache_attend.hip): pieces whose rows with one key head fit one
-//           such tile, and calls of too few rows to fill the device with
+//           such tile, and calls whose workgroups all run at once, or nearly;
 //   ROWS    128 rows a workgroup, whose waves take different rows and share the
-//           keys in LDS (cache_chunk.hip).  One piece, 16 heads, KEYS against
-//           ROWS: 1024 tokens (128 workgroups) 27.7 against 31.2 us, 2048 (256)
-//           39.9 against 33.5.
+//           keys in LDS (cache_chunk.hip).
+// Which of these two, by workgroups of ROWS in eighths of the CUs (a workgroup of
+// KEYS has a quarter of the rows; its registers leave room for three or four on a
+// CU at d = 32, two at 64, one at 128).  One piece, r = 128, KEYS against ROWS in
+// us, at 256 CUs:
+//   bf16, d = 32:   192 24.4 against 27.6, 224 28.5 against 28.3
+//         d = 64:   128 27.7 against 31.2, 144 34.3 against 32.2, 192 37.2 against 32.8
+//         d = 128:   64 36.8 against 41.4,  80 48.2 against 41.9, 192 66.4 against 44.2
+//   fp32, d = 64:   160 54.2 against 56.6, 192 61.2 against 57.9
+//         d = 128:  128 92.8 against 98.0, 144  110 against 98.6
 // The first two put new tokens into the cache as well, where no chunk is longer
 // than a block (the far field of such a chunk has nothing of its own).
 enum CacheRoute { CACHE_TOKENS, CACHE_KEYS, CACHE_ROWS };
@@ -94,13 +101,19 @@ inline ChunkShape chunk_shape(const CacheArgs &a)
 
 inline int token_rows(const CacheArgs &a) { return a.bf16 && a.head_dim <= 64 ? 2 : 4; }
 
+inline int keys_eighths(const CacheArgs &a)
+{
+    if (a.head_dim == 32) return 7;
+    return a.bf16 ? (a.head_dim == 64 ? 4 : 2) : (a.head_dim == 64 ? 5 : 4);
+}
+
 inline CacheRoute cache_route(const CacheArgs &a, int cus)
 {
     const long long most = a.max_chunk < a.rows ? a.max_chunk : a.rows;
     if (most * a.group <= token_rows(a)) return CACHE_TOKENS;
     const ChunkShape c = chunk_shape(a);
     const long long groups = (long long)a.rows * c.gs / (c.tm * c.gs < 128 ? c.tm * c.gs : 128) * a.kv_heads * c.split;
-    return most * c.gs <= 32 || groups < cus ? CACHE_KEYS : CACHE_ROWS;
+    return most * c.gs <= 32 || 8 * groups <= (long long)keys_eighths(a) * cus ? CACHE_KEYS : CACHE_ROWS;
 }
 
 // Workgroups are numbered tile by tile, a tile's key heads one after the other: a

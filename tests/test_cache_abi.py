@@ -235,20 +235,27 @@ def test_tiles_of_query_heads(tiling):
     out = (ctypes.c_int * 4)()
     for r in (16, 32, 64, 128, 192, 256):
         for group in range(1, 200):
-            tiling.host_cache_route(r, group, 1, r, 10 * r, 256, out)
+            tiling.host_cache_route(r, group, 1, r, 10 * r, 64, 1, 256, out)
             _, gs, split, tm = out[:]
             assert 1 <= gs <= 32 and (split - 1) * gs < group <= split * gs
             assert 1 <= tm <= r and tm * gs <= 128
             assert -(-r // tm) <= 2 * -(-r * gs // 128)
 
 
-@pytest.mark.parametrize("args,route", [
-    ((128, 1, 16, 1, 1), 0), ((128, 4, 4, 1, 100), 0), ((128, 1, 8, 4, 40), 0),    # up to four rows per key head
-    ((128, 5, 4, 1, 100), 1), ((128, 1, 16, 5, 2000), 1), ((128, 8, 16, 4, 9000), 1),   # one tile of 32
-    ((128, 1, 16, 128, 1024), 1), ((128, 1, 16, 4096, 2000), 1),                   # too few rows for the device
-    ((128, 1, 16, 128, 2048), 2), ((64, 4, 4, 2500, 8000), 2), ((16, 1, 16, 400, 400), 2)])
-def test_routes(tiling, args, route):
+BF32, BF64, BF128, F32, F64, F128 = (32, 1), (64, 1), (128, 1), (32, 0), (64, 0), (128, 0)
+
+
+@pytest.mark.parametrize("args,kind,route", [
+    ((128, 1, 16, 1, 1), BF64, 0), ((128, 2, 4, 1, 100), BF64, 0), ((128, 1, 8, 2, 40), BF32, 0),   # few rows per key head
+    ((128, 4, 4, 1, 100), BF128, 0), ((128, 1, 8, 4, 40), F64, 0), ((128, 4, 4, 1, 100), BF64, 1),
+    ((128, 5, 4, 1, 100), F128, 1), ((128, 1, 16, 5, 2000), BF64, 1), ((128, 8, 16, 4, 9000), BF128, 1),   # one tile of 32
+    ((128, 1, 16, 128, 1024), BF64, 1), ((128, 1, 16, 4096, 1792), BF32, 1), ((128, 1, 16, 4096, 512), BF128, 1),   # all at once
+    ((128, 1, 16, 4096, 1280), F64, 1), ((128, 1, 16, 4096, 1024), F128, 1), ((128, 1, 16, 4096, 1792), F32, 1),
+    ((128, 1, 16, 128, 1152), BF64, 2), ((128, 1, 16, 4096, 2048), BF32, 2), ((128, 1, 16, 4096, 640), BF128, 2),
+    ((128, 1, 16, 4096, 1536), F64, 2), ((128, 1, 16, 4096, 1152), F128, 2),
+    ((64, 4, 4, 2500, 8000), BF64, 2), ((16, 1, 16, 400, 400), BF64, 2)])
+def test_routes(tiling, args, kind, route):
     out = (ctypes.c_int * 4)()
     r, group, kv, chunk, rows = args
-    tiling.host_cache_route(r, group, kv, chunk, rows, 256, out)
+    tiling.host_cache_route(r, group, kv, chunk, rows, *kind, 256, out)
     assert out[0] == route
