@@ -508,8 +508,8 @@ fma_status_t fma_cache_attend(fma_cache_plan_t plan, const fma_cache_batch_t *ba
                               const fma_view_t *out, void *stream);
 
 /* fma_cache_append, then fma_cache_attend; in one launch where no sequence has
- * more than `block` new tokens and the rows are too few to fill the device with
- * tiles of 128.  A row always sees its own token here. */
+ * more than `block` new tokens and the call has few rows (about what the device
+ * holds at once).  A row always sees its own token here. */
 fma_status_t fma_cache_step(fma_cache_plan_t plan, const fma_cache_batch_t *batch, const fma_view_t *q,
                             const fma_view_t *k, const fma_view_t *v, const float *wk, const float *wv,
                             const fma_view_t *out, void *stream);
